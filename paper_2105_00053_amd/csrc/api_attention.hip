@@ -1,0 +1,208 @@
+// posit_attention_fwd / posit_attention_bwd: attention with a sliding window and sinks.
+#include "lm_codec.h"
+
+namespace pnn {
+
+struct Attn {
+    pnn_attention_desc d;
+    const void *q, *k, *v, *o, *d_o;
+    const int32_t* lens;
+    void *out, *copy, *dq, *dk, *dv;
+    float* lse;
+    const float* lse_in;
+    int kq, kkv, kout, kcopy, kd, ko;
+    ElemFmt fq, fkv, fout, fcopy, fd, fo;
+};
+
+__device__ __forceinline__ int64_t keys_of(const Attn& a, int64_t b) {
+    const int64_t n = a.lens ? a.lens[b] : a.d.LK;
+    return n < 0 ? 0 : (n > a.d.LK ? a.d.LK : n);
+}
+__device__ __forceinline__ bool sees(const Attn& a, int64_t p, int64_t j) { return j <= p && (a.d.window == 0 || j > p - a.d.window || j < a.d.sinks); }
+
+// One wave to a query: 64 keys at a time, one to a lane; then two of the head's elements to a lane.
+__global__ __launch_bounds__(64) void attn_fwd_simple(Attn a) {
+    __shared__ float qs[128], ps[64];
+    const pnn_attention_desc& d = a.d;
+    const int64_t i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, hk = h / (d.HQ / d.HKV);
+    const int t = threadIdx.x;
+    for (int c = t; c < d.D; c += 64) qs[c] = load_value(a.q, b * d.qb + i * d.ql + h * d.qh + c, a.kq, a.fq);
+    __syncthreads();
+    const float inf = f32_of_bits(0x7F800000u);
+    const int64_t p = keys_of(a, b) - d.LQ + i;
+    float m = -inf, l = 0.f, o[2] = {0.f, 0.f};
+    for (int64_t j0 = 0; j0 <= p; j0 += 64) {
+        const int64_t j = j0 + t;
+        float s = -inf;
+        if (j <= p && sees(a, p, j)) {
+            s = 0.f;
+            for (int c = 0; c < d.D; ++c) s = fmaf(qs[c], load_value(a.k, b * d.kb + j * d.kl + hk * d.kh + c, a.kkv, a.fkv), s);
+            s *= d.scale;
+        }
+        const float mt = wave_max(s), m1 = fmaxf(m, mt);
+        const bool nan = __any(s != s);
+        if (m1 == -inf && !nan) continue;
+        const float f = m == -inf ? 0.f : expf(m - m1), e = nan ? f32_of_bits(0x7FC00000u) : (s == -inf ? 0.f : expf(s - m1));
+        m = m1;
+        l = l * f + wave_sum(e);
+        __syncthreads();
+        ps[t] = e;
+        __syncthreads();
+        for (int c = 0; c < 2; ++c) {
+            if (t + 64 * c >= d.D) continue;
+            float acc = o[c] * f;
+            for (int jj = 0; jj < 64 && j0 + jj <= p; ++jj)
+                if (sees(a, p, j0 + jj)) acc = fmaf(ps[jj], load_value(a.v, b * d.vb + (j0 + jj) * d.vl + hk * d.vh + t + 64 * c, a.kkv, a.fkv), acc);
+            o[c] = acc;
+        }
+    }
+    const int64_t row = (b * d.LQ + i) * d.HQ + h;
+    for (int c = 0; c < 2; ++c)
+        if (t + 64 * c < d.D) {
+            const float v = l == 0.f ? 0.f : o[c] / l;
+            store_value(a.out, row * d.D + t + 64 * c, a.kout, a.fout, v);
+            if (a.copy) store_value(a.copy, row * d.D + t + 64 * c, a.kcopy, a.fcopy, v);
+        }
+    if (a.lse && t == 0) a.lse[(b * d.HQ + h) * d.LQ + i] = l == 0.f ? -inf : m + logf(l);
+}
+
+__device__ __forceinline__ float row_dot(const Attn& a, int64_t qat, const void* x, int kx, ElemFmt fx, int64_t kat, const void* y) {
+    float s = 0.f;
+    for (int c = 0; c < a.d.D; ++c) s = fmaf(load_value(x, qat + c, kx, fx), load_value(y, kat + c, a.kkv, a.fkv), s);
+    return s;
+}
+
+__device__ __forceinline__ float dot_with_o(const Attn& a, int64_t b, int64_t i, int64_t h) {
+    const pnn_attention_desc& d = a.d;
+    float s = 0.f;
+    for (int c = 0; c < d.D; ++c)
+        s = fmaf(load_value(a.d_o, b * d.qb + i * d.ql + h * d.qh + c, a.kd, a.fd), load_value(a.o, ((b * d.LQ + i) * d.HQ + h) * d.D + c, a.ko, a.fo), s);
+    return s;
+}
+
+__global__ __launch_bounds__(64) void attn_dq_simple(Attn a) {
+    __shared__ float ds[64];
+    const pnn_attention_desc& d = a.d;
+    const int64_t i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, hk = h / (d.HQ / d.HKV);
+    const int t = threadIdx.x;
+    const int64_t p = keys_of(a, b) - d.LQ + i, qat = b * d.qb + i * d.ql + h * d.qh;
+    const float lse = a.lse_in[(b * d.HQ + h) * d.LQ + i], dd = dot_with_o(a, b, i, h);
+    float g[2] = {0.f, 0.f};
+    for (int64_t j0 = 0; j0 <= p; j0 += 64) {
+        const int64_t j = j0 + t;
+        float e = 0.f;
+        if (j <= p && sees(a, p, j)) {
+            const float s = row_dot(a, qat, a.q, a.kq, a.fq, b * d.kb + j * d.kl + hk * d.kh, a.k) * d.scale;
+            e = expf(s - lse) * (row_dot(a, qat, a.d_o, a.kd, a.fd, b * d.vb + j * d.vl + hk * d.vh, a.v) - dd) * d.scale;
+        }
+        __syncthreads();
+        ds[t] = e;
+        __syncthreads();
+        for (int c = 0; c < 2; ++c)
+            if (t + 64 * c < d.D)
+                for (int jj = 0; jj < 64 && j0 + jj <= p; ++jj)
+                    if (sees(a, p, j0 + jj)) g[c] = fmaf(ds[jj], load_value(a.k, b * d.kb + (j0 + jj) * d.kl + hk * d.kh + t + 64 * c, a.kkv, a.fkv), g[c]);
+    }
+    for (int c = 0; c < 2; ++c)
+        if (t + 64 * c < d.D) store_value(a.dq, ((b * d.LQ + i) * d.HQ + h) * d.D + t + 64 * c, a.kout, a.fout, g[c]);
+}
+
+// One wave to a key: 64 queries at a time, over the heads that share it.
+__global__ __launch_bounds__(64) void attn_dkv_simple(Attn a) {
+    __shared__ float ps[64], ds[64];
+    const pnn_attention_desc& d = a.d;
+    const int64_t j = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const int t = threadIdx.x;
+    const int64_t n = keys_of(a, b), G = d.HQ / d.HKV;
+    float gk[2] = {0.f, 0.f}, gv[2] = {0.f, 0.f};
+    for (int64_t h = hk * G; h < hk * G + G; ++h)
+        for (int64_t i0 = 0; i0 < d.LQ && j < n; i0 += 64) {
+            const int64_t i = i0 + t, p = n - d.LQ + i, qat = b * d.qb + i * d.ql + h * d.qh;
+            float e = 0.f, w = 0.f;
+            if (i < d.LQ && sees(a, p, j)) {
+                const float s = row_dot(a, qat, a.q, a.kq, a.fq, b * d.kb + j * d.kl + hk * d.kh, a.k) * d.scale;
+                w = expf(s - a.lse_in[(b * d.HQ + h) * d.LQ + i]);
+                e = w * (row_dot(a, qat, a.d_o, a.kd, a.fd, b * d.vb + j * d.vl + hk * d.vh, a.v) - dot_with_o(a, b, i, h)) * d.scale;
+            }
+            __syncthreads();
+            ps[t] = w;
+            ds[t] = e;
+            __syncthreads();
+            for (int c = 0; c < 2; ++c)
+                if (t + 64 * c < d.D)
+                    for (int ii = 0; ii < 64 && i0 + ii < d.LQ; ++ii)
+                        if (sees(a, n - d.LQ + i0 + ii, j)) {
+                            const int64_t at = b * d.qb + (i0 + ii) * d.ql + h * d.qh + t + 64 * c;
+                            gk[c] = fmaf(ds[ii], load_value(a.q, at, a.kq, a.fq), gk[c]);
+                            gv[c] = fmaf(ps[ii], load_value(a.d_o, at, a.kd, a.fd), gv[c]);
+                        }
+        }
+    for (int c = 0; c < 2; ++c)
+        if (t + 64 * c < d.D) {
+            const int64_t at = ((b * d.LK + j) * d.HKV + hk) * d.D + t + 64 * c;
+            store_value(a.dk, at, a.kout, a.fout, gk[c]);
+            store_value(a.dv, at, a.kout, a.fout, gv[c]);
+        }
+}
+
+// formats that bfloat16 holds exactly: at most 8 significant bits
+inline int operand_status(int f) {
+    if (const int s = element_status(f)) return s;
+    return f == PNN_POSIT16_1 || f == PNN_POSIT12_1 || f == PNN_F32 ? PNN_EUNSUPPORTED : PNN_OK;
+}
+
+inline int desc_status(const pnn_attention_desc* d) {
+    if (!d || d->B < 0 || d->HQ < 0 || d->HKV < 0 || d->LQ < 0 || d->LK < 0 || d->D < 0 || d->window < 0 || d->sinks < 0) return PNN_EINVAL;
+    if ((d->HKV == 0) != (d->HQ == 0) || (d->HKV > 0 && d->HQ % d->HKV != 0)) return PNN_EINVAL;
+    if (!(d->scale > -3.4028235e38f && d->scale < 3.4028235e38f)) return PNN_EINVAL;
+    if (d->qb < 0 || d->ql < 0 || d->qh < 0 || d->kb < 0 || d->kl < 0 || d->kh < 0 || d->vb < 0 || d->vl < 0 || d->vh < 0) return PNN_EINVAL;
+    const int64_t most = (int64_t)1 << 31;
+    if (d->D > 128 || d->LQ >= most || d->LK >= most || d->HQ >= 65536 || d->B >= 65536) return PNN_EUNSUPPORTED;
+    return PNN_OK;
+}
+
+}  // namespace pnn
+
+using namespace pnn;
+
+extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attention_desc* desc) { return 0; }
+
+extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, const pnn_attention_desc* desc, const void* q, const void* k, const void* v,
+                                   const int32_t* lens, void* o, float* lse, int fcopy, void* o_copy, void* workspace, size_t workspace_bytes) {
+    if (const int s = desc_status(desc)) return s;
+    for (int f : {fq, fkv})
+        if (const int s = operand_status(f)) return s;
+    for (int f : {fout, o_copy ? fcopy : fout})
+        if (const int s = element_status(f)) return s;
+    const pnn_attention_desc& d = *desc;
+    if (d.B == 0 || d.HQ == 0 || d.LQ == 0 || d.D == 0) return PNN_OK;
+    if (!q || !o || (d.LK > 0 && (!k || !v))) return PNN_EINVAL;
+    discard_stale_hip_error();
+    Attn a = {};
+    a.d = d; a.q = q; a.k = k; a.v = v; a.lens = lens; a.out = o; a.copy = o_copy; a.lse = lse;
+    a.kq = kind_of(fq); a.fq = elem_fmt(fq); a.kkv = kind_of(fkv); a.fkv = elem_fmt(fkv); a.kout = kind_of(fout); a.fout = elem_fmt(fout);
+    a.kcopy = kind_of(o_copy ? fcopy : fout); a.fcopy = elem_fmt(o_copy ? fcopy : fout);
+    hipLaunchKernelGGL(attn_fwd_simple, dim3((unsigned)d.LQ, (unsigned)d.HQ, (unsigned)d.B), dim3(64), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+}
+
+extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo, int fout, const pnn_attention_desc* desc, const void* d_o, const void* q,
+                                   const void* k, const void* v, const int32_t* lens, const void* o, const float* lse, void* dq, void* dk, void* dv,
+                                   void* workspace, size_t workspace_bytes) {
+    if (const int s = desc_status(desc)) return s;
+    for (int f : {fd, fq, fkv})
+        if (const int s = operand_status(f)) return s;
+    for (int f : {fo, fout})
+        if (const int s = element_status(f)) return s;
+    const pnn_attention_desc& d = *desc;
+    if (d.B == 0 || d.HQ == 0 || d.D == 0 || (d.LQ == 0 && d.LK == 0)) return PNN_OK;
+    if ((d.LQ > 0 && (!d_o || !q || !o || !lse || !dq)) || (d.LK > 0 && (!k || !v || !dk || !dv))) return PNN_EINVAL;
+    discard_stale_hip_error();
+    Attn a = {};
+    a.d = d; a.q = q; a.k = k; a.v = v; a.d_o = d_o; a.o = o; a.lse_in = lse; a.lens = lens; a.dq = dq; a.dk = dk; a.dv = dv;
+    a.kq = kind_of(fq); a.fq = elem_fmt(fq); a.kkv = kind_of(fkv); a.fkv = elem_fmt(fkv); a.kout = kind_of(fout); a.fout = elem_fmt(fout);
+    a.kd = kind_of(fd); a.fd = elem_fmt(fd); a.ko = kind_of(fo); a.fo = elem_fmt(fo);
+    if (d.LQ > 0) hipLaunchKernelGGL(attn_dq_simple, dim3((unsigned)d.LQ, (unsigned)d.HQ, (unsigned)d.B), dim3(64), 0, (hipStream_t)stream, a);
+    if (d.LK > 0) hipLaunchKernelGGL(attn_dkv_simple, dim3((unsigned)d.LK, (unsigned)d.HKV, (unsigned)d.B), dim3(64), 0, (hipStream_t)stream, a);
+    return hip_status(hipGetLastError());
+}

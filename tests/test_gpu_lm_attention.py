@@ -1,0 +1,269 @@
+"""Attention with a sliding window and sinks, forward and backward, against plain forms in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2105_00053_amd as pn
+from lm_util import attention, check, normal, to_format, values
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+OPERANDS = ["p8", "p8_1", "p8_2", "p10_1", "p10_2", "p12_2", "bf16"]
+
+
+def _bits(fout):
+    return 8 if fout == "bf16" else 16
+
+
+def _inputs(b, lq, lk, hq, hkv, d, fq, fkv, seed=0):
+    rng = np.random.default_rng([seed, b, lq, lk, hq, d])
+    return (rng, to_format(normal(rng, (b, lq, hq, d), 1.5), fq), to_format(normal(rng, (b, lk, hkv, d)), fkv), to_format(normal(rng, (b, lk, hkv, d)), fkv),
+            to_format(normal(rng, (b, lq, hq, d)), fq))
+
+
+def _compare(q, k, v, do, fq, fkv, fout, window=0, sinks=0, lens=None, scale=None, back=True, fcopy="f32"):
+    b, lq, hq, d = q.shape
+    lk = k.shape[1]
+    scale = 1 / np.sqrt(d) if scale is None else scale
+    lt = None if lens is None else torch.from_numpy(np.asarray(lens, np.int32)).cuda()
+    o, lse, copy = pn.posit_attention_fwd(q, k, v, fq, fkv, fout, scale=scale, window=window, sinks=sinks, lens=lt, fcopy=fcopy)
+    s32 = np.float64(np.float32(scale))
+    ln = [lk] * b if lens is None else lens
+    w = attention(values(q, fq), values(k, fkv), values(v, fkv), s32, window, sinks, ln, _bits(fout), values(do, fq) if back else None, _bits(fout))
+    check(lse, w["lse"], w["s_lse"], "f32", "lse")
+    check(o, w["o"], w["s_o"], fout, "o")
+    if copy is not None:
+        check(copy, w["o"], w["s_o"], fcopy, "o_copy")
+    if back:
+        dq, dk, dv = pn.posit_attention_bwd(do, q, k, v, copy, lse, fq, fq, fkv, fcopy, fout, scale=scale, window=window, sinks=sinks, lens=lt)
+        for n, t in (("dv", dv), ("dq", dq), ("dk", dk)):
+            check(t, w[n], w["s_" + n], fout, n)
+    return o, lse, copy
+
+
+@pytest.mark.parametrize("lq,lk", [(1, 1), (2, 2), (1, 31), (5, 5), (31, 31), (32, 32), (33, 33), (63, 64), (65, 65), (7, 130), (100, 129), (130, 130), (200, 257)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_lengths(lq, lk, d):
+    _, q, k, v, do = _inputs(1, lq, lk, 2, 1, d, "bf16", "p8_1", 1)
+    _compare(q, k, v, do, "bf16", "p8_1", "bf16")
+    _compare(q, k, v, do, "bf16", "p8_1", "f32", window=40, sinks=3)
+
+
+@pytest.mark.parametrize("d", [1, 2, 7, 8, 16, 17, 32, 33, 40, 48, 63, 65, 72, 80, 96, 100, 112, 127, 128])
+def test_head_sizes(d):
+    _, q, k, v, do = _inputs(2, 37, 70, 4, 2, d, "p8_1", "p8_2", 2)
+    _compare(q, k, v, do, "p8_1", "p8_2", "bf16", lens=[70, 45])
+    _compare(q[:, :1], k, v, do[:, :1], "p8_1", "p8_2", "f32", lens=[70, 45], window=16, sinks=2)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 3), (4, 2), (5, 1), (8, 1), (12, 4), (40, 1), (33, 1)])
+@pytest.mark.parametrize("lq", [1, 3, 45])
+def test_shared_heads(hq, hkv, lq):
+    _, q, k, v, do = _inputs(2, lq, 90, hq, hkv, 64, "p8_2", "p8_2", 3)
+    _compare(q, k, v, do, "p8_2", "p8_2", "bf16", lens=[90, 51], window=33, sinks=1)
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (2, 5), (16, 4), (63, 0), (64, 64), (65, 3), (100, 0), (129, 16), (500, 4), (0, 7), (30, 300), (10, 200)])
+@pytest.mark.parametrize("lq,lk", [(1, 300), (6, 300), (300, 300)])
+def test_windows_and_sinks(window, sinks, lq, lk):
+    _, q, k, v, do = _inputs(1, lq, lk, 2, 1, 64, "p8_1", "p8_1", 4)
+    _compare(q, k, v, do, "p8_1", "p8_1", "bf16", window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("lq", [1, 2, 17, 96])
+def test_ragged_lengths_and_empty_rows(lq):
+    """Sequences without keys, of one key, shorter than their queries, and with lengths out of range."""
+    lens = [0, 1, lq, max(0, lq - 3), 96, 95, 64, 33]
+    _, q, k, v, do = _inputs(8, lq, 96, 2, 2, 64, "p8_2", "p8_1", 5)
+    o, lse, _ = _compare(q, k, v, do, "p8_2", "p8_1", "bf16", lens=lens)
+    assert (o[0] == 0).all() and torch.isinf(lse[0]).all()
+    _compare(q, k, v, do, "p8_2", "p8_1", "p8", lens=lens, window=7, sinks=2)
+    wild = list(lens)
+    wild[0], wild[4] = -5, 1000
+    a = _compare(q, k, v, do, "p8_2", "p8_1", "bf16", lens=wild)
+    assert torch.equal(a[0], o) and torch.equal(a[1], lse)
+
+
+@pytest.mark.parametrize("fq", OPERANDS)
+@pytest.mark.parametrize("fkv", OPERANDS)
+def test_formats(fq, fkv):
+    for lq, fout in ((1, "p8_1"), (1, "f32"), (40, "bf16"), (40, "p16"), (40, "p12_1")):
+        _, q, k, v, do = _inputs(1, lq, 70, 2, 1, 48, fq, fkv, 6)
+        _compare(q, k, v, do, fq, fkv, fout, window=50, sinks=2, fcopy="f32" if fout != "f32" else "p16", back=fout != "f32")
+
+
+@pytest.mark.parametrize("b,lk,hq,hkv,d,window,sinks", [(3, 2000, 8, 2, 64, 0, 0), (2, 5000, 4, 1, 128, 700, 4), (1, 9001, 8, 8, 96, 0, 0), (5, 1500, 10, 2, 40, 64, 1)])
+def test_single_tokens_on_long_caches(b, lk, hq, hkv, d, window, sinks):
+    _, q, k, v, do = _inputs(b, 1, lk, hq, hkv, d, "bf16", "p8_1", 7)
+    lens = [lk - 37 * i - i * i for i in range(b)]
+    _compare(q, k, v, do, "bf16", "p8_1", "bf16", window=window, sinks=sinks, lens=lens, back=False)
+    _compare(q, k, v, do, "bf16", "p8_1", "p8_1", window=window, sinks=sinks, lens=lens, back=False)
+
+
+def test_large_and_small_scores():
+    """Scores far apart, all equal, and a scale of zero and below."""
+    rng, q, k, v, do = _inputs(1, 40, 80, 2, 1, 64, "bf16", "bf16", 8)
+    _compare(q * 30, k, v, do, "bf16", "bf16", "bf16")
+    _compare(q * 0, k, v, do, "bf16", "bf16", "bf16", window=20)
+    for scale in (0.0, -0.2):
+        _compare(q, k, v, do, "bf16", "bf16", "f32", scale=scale)
+        _compare(q[:, :1], k, v, do[:, :1], "bf16", "bf16", "f32", scale=scale)
+
+
+def test_strided_views_and_other_streams():
+    """q, k and v as slices of one product's rows, a cache with heads outside positions, odd offsets."""
+    rng = np.random.default_rng(9)
+    b, l, hq, hkv, d = 2, 50, 4, 2, 40
+    for fmt in ("p8_1", "bf16"):
+        rows = to_format(normal(rng, (b, l, (hq + 2 * hkv) * d + 3)), fmt)
+        q = rows[:, :, 1:1 + hq * d].unflatten(2, (hq, d))
+        k = rows[:, :, 1 + hq * d:1 + (hq + hkv) * d].unflatten(2, (hkv, d))
+        v = rows[:, :, 1 + (hq + hkv) * d:1 + (hq + 2 * hkv) * d].unflatten(2, (hkv, d))
+        cache = to_format(normal(rng, (b, hkv, l, d)), fmt).permute(0, 2, 1, 3)
+        do = to_format(normal(rng, (b, l, hq, d)), fmt)
+        for kk, vv, qq, dd in ((k, v, q, do), (cache, v, q, do), (cache, cache, q[:, :1], do[:, :1])):
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                x = pn.posit_attention_fwd(qq, kk, vv, fmt, fmt, "bf16", window=20, sinks=2, fcopy="f32")
+                gx = pn.posit_attention_bwd(dd, qq, kk, vv, x[2], x[1], fmt, fmt, fmt, "f32", "bf16", window=20, sinks=2)
+            side.synchronize()
+            y = pn.posit_attention_fwd(qq.contiguous(), kk.contiguous(), vv.contiguous(), fmt, fmt, "bf16", window=20, sinks=2, fcopy="f32")
+            gy = pn.posit_attention_bwd(dd, qq.contiguous(), kk.contiguous(), vv.contiguous(), y[2], y[1], fmt, fmt, fmt, "f32", "bf16", window=20, sinks=2)
+            assert all(torch.equal(s, t) for s, t in zip(x + gx, y + gy))
+
+
+@pytest.mark.parametrize("lq", [1, 4, 70])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_nar_reaches_only_what_sees_it(lq, where):
+    lk, window, sinks = 150, 20, 3
+    for at in (1, 60, 128, 149):
+        _, q, k, v, do = _inputs(2, lq, lk, 4, 2, 64, "p8_1", "p8_1", 10)
+        t = k if where == "k" else v
+        t[0, at, 1, 5] = 128  # NaR
+        t[0, at, 1, 33] = 128
+        lens = [lk, 100]
+        lt = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        for fout in ("bf16", "p8_1"):
+            o, lse, _ = pn.posit_attention_fwd(q, k, v, "p8_1", "p8_1", fout, window=window, sinks=sinks, lens=lt)
+            w = attention(values(q, "p8_1"), values(k, "p8_1"), values(v, "p8_1"), np.float64(np.float32(1 / 8)), window, sinks, lens, _bits(fout))
+            check(lse, w["lse"], w["s_lse"], "f32", "lse")
+            check(o, w["o"], w["s_o"], fout, "o")
+
+
+def test_infinities_in_values_reach_only_what_sees_them():
+    lk = 140
+    for lq in (1, 70):
+        _, q, k, v, do = _inputs(1, lq, lk, 2, 1, 64, "bf16", "bf16", 11)
+        v[0, 100, 0, 3], v[0, 101, 0, 3], v[0, 102, 0, 4], v[0, 103, 0, 9] = INF, -INF, INF, -INF
+        v[0, 139, 0, 20] = float("nan")
+        for window in (5, 39, 0):
+            o, lse, _ = pn.posit_attention_fwd(q, k, v, "bf16", "bf16", "bf16", window=window)
+            w = attention(values(q, "bf16"), values(k, "bf16"), values(v, "bf16"), 0.125, window, 0, [lk], 8)
+            check(o, w["o"], w["s_o"], "bf16", "o")
+            check(lse, w["lse"], w["s_lse"], "f32", "lse")
+
+
+@pytest.mark.parametrize("where", ["do", "q", "k", "v"])
+def test_nar_in_the_backward_pass(where):
+    """Which gradients a NaR reaches: those of the pairs of a query and a key that see each other."""
+    b, l, h, d, window = 1, 100, 2, 64, 16
+    for at in (0, 50, 99):
+        _, q, k, v, do = _inputs(b, l, l, h, 1, d, "p8_1", "p8_1", 12)
+        clean = [t.clone() for t in (do, q, k, v)]
+        {"do": do, "q": q, "k": k, "v": v}[where][0, at, 0, 7] = 128
+        grads = []
+        for dd, qq, kk, vv in ((do, q, k, v), tuple(clean)):
+            o, lse, copy = pn.posit_attention_fwd(qq, kk, vv, "p8_1", "p8_1", "bf16", window=window, fcopy="f32")
+            grads.append([values(t, "bf16") for t in pn.posit_attention_bwd(dd, qq, kk, vv, copy, lse, "p8_1", "p8_1", "p8_1", "f32", "bf16", window=window)])
+        i = np.arange(l)
+        rows = np.zeros((l, h), bool)  # queries whose scores or score gradients are NaN
+        if where in ("do", "q"):
+            rows[at, 0] = True
+        else:
+            rows[(i >= at) & (i < at + window)] = True
+        # P is NaN for the rows whose scores are; a NaN in v or do reaches dS only
+        scores = rows if where in ("q", "k") else np.zeros_like(rows)
+        wq = np.repeat(rows[:, :, None], d, 2)
+        wk, wv = np.zeros((l, d), bool), np.zeros((l, d), bool)
+        for p, hh in np.argwhere(rows):
+            wk[max(0, p - window + 1):p + 1] = True
+        for p, hh in np.argwhere(scores):
+            wv[max(0, p - window + 1):p + 1] = True
+        if where == "do":
+            wv[max(0, at - window + 1):at + 1, 7] = True
+        for n, got, ref, want in (("dq", grads[0][0][0], grads[1][0][0], wq), ("dk", grads[0][1][0, :, 0], grads[1][1][0, :, 0], wk),
+                                  ("dv", grads[0][2][0, :, 0], grads[1][2][0, :, 0], wv)):
+            assert np.array_equal(np.isnan(got), want), (n, at, np.argwhere(np.isnan(got) != want)[:5])
+            assert np.array_equal(got[~want], ref[~want]), (n, at)
+
+
+def test_gradient_against_differences():
+    rng, q, k, v, do = _inputs(1, 9, 12, 2, 1, 8, "bf16", "bf16", 13)
+    o, lse, copy = pn.posit_attention_fwd(q, k, v, "bf16", "bf16", "f32", scale=0.5, window=6, sinks=1, fcopy="f32")
+    got = [values(t, "f32") for t in pn.posit_attention_bwd(do, q, k, v, copy, lse, "bf16", "bf16", "bf16", "f32", "f32", scale=0.5, window=6, sinks=1)]
+    base = [values(t, "bf16") for t in (q, k, v)]
+    g = values(do, "bf16")
+
+    def loss(x):
+        return (g * attention(x[0], x[1], x[2], 0.5, 6, 1, [12], 16)["o"]).sum()
+
+    for n in range(3):
+        for _ in range(6):
+            at = tuple(rng.integers(0, s) for s in base[n].shape)
+            d = [np.zeros_like(x) for x in base]
+            d[n][at] = 1e-4
+            diff = (loss([x + e for x, e in zip(base, d)]) - loss([x - e for x, e in zip(base, d)])) / 2e-4
+            # probabilities to 16 bits and differences to about 1e-8
+            assert abs(diff - got[n][at]) < 2e-4 * (1 + abs(diff)), (n, at)
+
+
+def test_repeats_are_identical_and_workspaces_are_shared():
+    _, q, k, v, do = _inputs(2, 150, 150, 4, 2, 64, "p8_1", "p8_1", 14)
+    first = None
+    ws = torch.full((pn.posit_attention_workspace(1, "p8_1", pn.AttentionDesc(2, 4, 2, 150, 150, 64, 0, 0, 0.125, 1, 1, 1, 1, 1, 1, 1, 1, 1)) + 4096,), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        o, lse, copy = pn.posit_attention_fwd(q, k, v, "p8_1", "p8_1", "bf16", fcopy="f32", workspace=ws)
+        g = pn.posit_attention_bwd(do, q, k, v, copy, lse, "p8_1", "p8_1", "p8_1", "f32", "bf16", workspace=ws)
+        out = (o, lse, copy) + tuple(g)
+        if first is not None:
+            assert all(torch.equal(a, b) for a, b in zip(first, out))
+        first = out
+
+
+def test_offsets_beyond_32_bits():
+    """The last sequence of a cache of more than 2^32 elements."""
+    b, lk, hkv, d = 9, 4 * 1024 * 1024, 1, 128
+    cache = torch.zeros((b, lk, hkv, d), dtype=torch.uint8, device="cuda")
+    n = 300
+    rng, q, k, v, _ = _inputs(1, 1, n, 2, 1, d, "bf16", "p8_1", 15)
+    lens = torch.full((b,), n, dtype=torch.int32, device="cuda")
+    cache[-1, :n] = k[0]
+    cache[-1, n:2 * n] = v[0]
+    qq = q.expand(b, 1, 2, d).contiguous()
+    o, lse, _ = pn.posit_attention_fwd(qq, cache[:, :n], cache[:, n:2 * n], "bf16", "p8_1", "f32", lens=lens)
+    want, wlse, _ = pn.posit_attention_fwd(q, k, v, "bf16", "p8_1", "f32")
+    assert torch.equal(o[-1], want[0]) and torch.equal(lse[-1], wlse[0])
+    # and the last keys of one sequence that long: a window on its end
+    one = cache.view(1, b * lk, hkv, d)
+    one[0, -n:] = k[0]
+    o, lse, _ = pn.posit_attention_fwd(q, one, one, "bf16", "p8_1", "f32", window=n)
+    want, wlse, _ = pn.posit_attention_fwd(q, k, k, "bf16", "p8_1", "f32")
+    assert (o - want).abs().max() < 1e-4 and (lse - wlse).abs().max() < 1e-5
+
+
+def test_empty():
+    q = torch.empty((2, 0, 2, 64), dtype=torch.uint8, device="cuda")
+    k = torch.zeros((2, 5, 1, 64), dtype=torch.uint8, device="cuda")
+    o, lse, _ = pn.posit_attention_fwd(q, k, k, "p8", "p8", "bf16")
+    assert o.shape == (2, 0, 2, 64)
+    o32 = torch.empty((2, 0, 2, 64), device="cuda")
+    dq, dk, dv = pn.posit_attention_bwd(q, q, k, k, o32, lse, "p8", "p8", "p8", "f32", "bf16")
+    assert (dk == 0).all() and (dv == 0).all()
+    q = torch.zeros((2, 3, 2, 64), dtype=torch.uint8, device="cuda")
+    k = torch.empty((2, 0, 1, 64), dtype=torch.uint8, device="cuda")
+    o, lse, c = pn.posit_attention_fwd(q, k, k, "p8", "p8", "bf16", fcopy="f32")
+    assert (o == 0).all() and torch.isinf(lse).all()
+    dq, dk, dv = pn.posit_attention_bwd(q, q, k, k, c, lse, "p8", "p8", "p8", "f32", "bf16")
+    assert (dq == 0).all() and dk.shape == (2, 0, 1, 64)
