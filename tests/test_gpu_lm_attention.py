@@ -222,7 +222,9 @@ def test_gradient_against_differences():
 def test_repeats_are_identical_and_workspaces_are_shared():
     _, q, k, v, do = _inputs(2, 150, 150, 4, 2, 64, "p8_1", "p8_1", 14)
     first = None
-    ws = torch.full((pn.posit_attention_workspace(1, "p8_1", pn.AttentionDesc(2, 4, 2, 150, 150, 64, 0, 0, 0.125, 1, 1, 1, 1, 1, 1, 1, 1, 1)) + 4096,), 255, dtype=torch.uint8, device="cuda")
+    desc = pn.AttentionDesc(2, 4, 2, 150, 150, 64, 0, 0, 0.125, 1, 1, 1, 1, 1, 1, 1, 1, 1)
+    need = max(pn.posit_attention_workspace(which, "p8_1", desc) for which in (0, 1))
+    ws = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
     for _ in range(3):
         o, lse, copy = pn.posit_attention_fwd(q, k, v, "p8_1", "p8_1", "bf16", fcopy="f32", workspace=ws)
         g = pn.posit_attention_bwd(do, q, k, v, copy, lse, "p8_1", "p8_1", "p8_1", "f32", "bf16", workspace=ws)
