@@ -1,0 +1,275 @@
+// Gradients of attention, from recomputed probabilities: P = exp(S - lse), dS = P * (dP - D) with dP = dO V^T and D = rowsum(dO * o).
+//
+// Two kernels, so that every sum has one owner and a fixed order (no atomics): one walks the keys of 128 rows (dQ), as the forward kernel
+// does; one walks the rows that see 128 keys (dK and dV), where the heads that share a key are rows like others.  In both
+// the products that reduce over a head's elements come out in the lane order that the next product wants its operand in.
+//   rows:  S^T = K Q^T and dP^T = V dO^T (a lane holds one row: lse and D are its own), dQ^T += K^T dS^T
+//   keys:  S = Q K^T and dP = dO V^T (a lane holds one key), dV^T += dO^T P, dK^T += Q^T dS
+#pragma once
+
+#include "attn_prompt.h"
+
+namespace pnn {
+
+// What the kernels need to know of each row, by blocks of 32: lse in powers of two, D, position (-1 behind the last row).
+constexpr int AT_STATS = 96;
+
+struct AttnBwd {
+    AttnShape s;
+    const uint4 *q, *k, *v, *g;   // row fragments
+    const uint4 *qt, *kt, *gt;    // transposed fragments
+    const float* stats;
+    void *dq, *dk, *dv;
+    int kout;
+    ElemFmt fout;
+    int nbh;
+    const int32_t* flags;         // of d_o's blocks, and d_o itself for those
+    const void* gsrc;
+    int64_t gb, gl, gh;
+    int kg;
+    ElemFmt fg;
+};
+
+struct AttnStats {
+    AttnShape s;
+    const void *g, *o;
+    int64_t gb, gl, gh;
+    const float* lse;
+    float* stats;
+    int kg, ko;
+    ElemFmt fg, fo;
+};
+
+// Eight lanes to a row, 32 rows to a workgroup.
+__global__ __launch_bounds__(256) void attn_stats_kernel(AttnStats a) {
+    const AttnShape& s = a.s;
+    const int t = threadIdx.x, blk = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, r = t >> 3, row = blk * 32 + r;
+    const int i = row / s.G, h = hk * s.G + (row - i * s.G), HQ = s.HKV * s.G;
+    const bool live = row < s.rows;
+    float d = 0.f;
+    if (live) {
+        const int64_t ga = b * a.gb + i * a.gl + h * a.gh, oa = (((int64_t)b * s.LQ + i) * HQ + h) * s.D;
+        for (int e = t & 7; e < s.D; e += 8) d = fmaf(load_value(a.g, ga + e, a.kg, a.fg), load_value(a.o, oa + e, a.ko, a.fo), d);
+    }
+#pragma unroll
+    for (int m = 4; m >= 1; m >>= 1) d += __shfl_xor(d, m, 64);
+    float* const out = a.stats + (((int64_t)b * s.HKV + hk) * s.qblocks + blk) * AT_STATS + r;
+    if ((t & 7) == 0) {
+        out[0] = live ? a.lse[((int64_t)b * HQ + h) * s.LQ + i] * 1.4426950408889634f : 0.f;
+        out[32] = d;
+        out[64] = __builtin_bit_cast(float, live ? at_keys(s, b) - s.LQ + i : -1);
+    }
+}
+
+template <int DB, bool TWO>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
+    constexpr int KS = 2 * DB, RUNS = 3 * KS;  // 1 KB runs of a tile of 32 keys: keys, values, keys transposed
+    __shared__ uint4 buf[2][RUNS * 64];
+    const AttnShape& s = a.s;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = gridDim.x / (unsigned)a.nbh - 1 - blockIdx.x / (unsigned)a.nbh;
+    const int b = bh / s.HKV, hk = bh - b * s.HKV, base = at_keys(s, b) - s.LQ;
+    const int r0 = tile * 128, rw = r0 + w * 32, row = rw + (lane & 31);
+    const int last = (r0 + 128 < s.rows ? r0 + 128 : s.rows) - 1;
+    const int i = row / s.G;
+    const bool live = row < s.rows;
+    const int p = live ? base + i : -1, low = s.window ? p - s.window : -1;
+    const AttnTiles tiles = at_tiles<32>(s, base + r0 / s.G, base + last / s.G);
+    const int wlast = rw + 31 < last ? rw + 31 : last;
+    const int wp0 = base + rw / s.G, wp1 = rw <= last ? base + wlast / s.G : -1;
+    const int wlow0 = s.window ? wp0 - s.window : -1, wlow1 = s.window ? wp1 - s.window : -1;
+    const float c = s.scale * 1.4426950408889634f;
+
+    at_v8b q[KS], g[KS];
+    const int64_t mine = (int64_t)bh * s.qblocks + tile * 4 + w;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        q[ks] = at_frag(a.q[(mine * KS + ks) * 64 + lane]);
+        g[ks] = at_frag(a.g[(mine * KS + ks) * 64 + lane]);
+    }
+    const float lse = a.stats[mine * AT_STATS + (lane & 31)], dd = a.stats[mine * AT_STATS + 32 + (lane & 31)];
+
+    const uint4* const src[3] = {a.k + (int64_t)bh * s.kblocks * (KS * 64), a.v + (int64_t)bh * s.kblocks * (KS * 64), a.kt + (int64_t)bh * s.kblocks * (KS * 64)};
+    auto issue = [&](int n) {
+        const int64_t at = (int64_t)tiles.at(n) * (KS * 64);
+        uint4* dst = buf[n & 1];
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+#pragma unroll
+            for (int r = 0; r < KS; r += 4)
+                if (r + w < KS) at_copy(src[x] + at + (r + w) * 64, dst + (x * KS + r + w) * 64, lane);
+    };
+
+    at_v16f dq[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dq[d] = at_zero();
+    if (tiles.count > 0) issue(0);
+    for (int n = 0; n < tiles.count; ++n) {
+        at_landed();
+        if (n + 1 < tiles.count) issue(n + 1);
+        const int key0 = tiles.at(n) * 32;
+        if (!(key0 <= wp1 && (key0 + 31 > wlow0 || key0 < s.sinks))) continue;
+        const uint4* kb = buf[n & 1] + lane;
+        at_v16f sc = at_zero(), dp = at_zero();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc = at_mfma(at_frag(kb[ks * 64]), q[ks], sc);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = at_mfma(at_frag(kb[(KS + ks) * 64]), g[ks], dp);
+        const bool whole = key0 + 31 <= wp0 && (key0 > wlow1 || key0 + 31 < s.sinks);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -lse)) * (dp[r] - dd);
+        if (!whole) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[r] = at_sees(s, p, low, key0 + at_row(r, half)) ? sc[r] : 0.f;
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const at_v8b sh = at_round(sc, 8 * y);
+            at_v8b sl;
+            if (TWO) sl = at_rest(sc, 8 * y, sh);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const at_v8b k = at_frag(kb[(2 * KS + y * DB + d) * 64]);
+                dq[d] = at_mfma(k, sh, dq[d]);
+                if (TWO) dq[d] = at_mfma(k, sl, dq[d]);
+            }
+        }
+    }
+    if (!live) return;
+    const int64_t at = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + hk * s.G + (row - i * s.G)) * s.D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int e = d * 32 + at_row(r, half);
+            if (e < s.D) store_value(a.dq, at + e, a.kout, a.fout, dq[d][r] * s.scale);
+        }
+}
+
+// Four waves, 32 keys each; one block of 32 rows at a time.
+template <int DB, bool TWO>
+__global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd a) {
+    constexpr int KS = 2 * DB, RUNS = 4 * KS;  // 1 KB runs of a block of rows: q, d_o, both transposed
+    __shared__ uint4 buf[2][RUNS * 64];
+    __shared__ __attribute__((aligned(16))) float stats[2][AT_STATS];
+    const AttnShape& s = a.s;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh;
+    const int b = bh / s.HKV, hk = bh - b * s.HKV, keys = at_keys(s, b), base = keys - s.LQ;
+    const int k0 = tile * 128, kw = k0 + w * 32, key = kw + (lane & 31);
+    const float c = s.scale * 1.4426950408889634f;
+    // the rows that see any of the workgroup's keys: from the position of its first key to the end of its last key's window
+    const int i0 = k0 - base > 0 ? k0 - base : 0;
+    int64_t i1 = s.LQ - 1;
+    if (s.window && k0 >= s.sinks && (int64_t)k0 + 126 + s.window - base < i1) i1 = (int64_t)k0 + 126 + s.window - base;
+    const int first = (int)((int64_t)i0 * s.G / 32), blocks = k0 >= keys || i0 > i1 ? 0 : (int)((i1 * s.G + s.G - 1) / 32) - first + 1;
+
+    at_v8b kf[KS], vf[KS];
+    const int64_t mine = (int64_t)bh * s.kblocks + tile * 4 + w;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        kf[ks] = at_frag(a.k[(mine * KS + ks) * 64 + lane]);
+        vf[ks] = at_frag(a.v[(mine * KS + ks) * 64 + lane]);
+    }
+    const int64_t rows0 = (int64_t)bh * s.qblocks;
+    const uint4* const src = (w == 0 ? a.q : w == 1 ? a.g : w == 2 ? a.qt : a.gt) + rows0 * (KS * 64);
+    auto issue = [&](int n) {
+        const int64_t at = (int64_t)(first + n) * (KS * 64);
+        uint4* dst = buf[n & 1] + w * (KS * 64);
+#pragma unroll
+        for (int r = 0; r < KS; ++r) at_copy(src + at + r * 64, dst + r * 64, lane);
+        if (w == 0 && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + first + n) * AT_STATS), (uint4*)stats[n & 1], lane);
+    };
+
+    at_v16f dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        dk[d] = at_zero();
+        dv[d] = at_zero();
+    }
+    if (blocks > 0) issue(0);
+    for (int n = 0; n < blocks; ++n) {
+        at_landed();
+        if (n + 1 < blocks) issue(n + 1);
+        const uint4* rb = buf[n & 1] + lane;
+        const float* st = stats[n & 1];
+        const int row0 = (first + n) * 32;
+        const int p0 = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[64]));
+        const int p1 = row0 + 31 < s.rows ? __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[95])) : base + s.LQ - 1;
+        const int low0 = s.window ? p0 - s.window : -1, low1 = s.window ? p1 - s.window : -1;
+        if (!(kw <= p1 && (kw + 31 > low0 || kw < s.sinks))) continue;
+        const bool whole = kw + 31 <= p0 && (kw > low1 || kw + 31 < s.sinks) && row0 + 31 < s.rows;
+        at_v16f sc = at_zero(), dp = at_zero();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc = at_mfma(at_frag(rb[ks * 64]), kf[ks], sc);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = at_mfma(at_frag(rb[(KS + ks) * 64]), vf[ks], dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -st[at_row(r, half)]));
+        if (!whole) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int p = __builtin_bit_cast(int, st[64 + at_row(r, half)]);
+                const bool see = at_sees(s, p, s.window ? p - s.window : -1, key);
+                sc[r] = see ? sc[r] : 0.f;
+                dp[r] = see ? dp[r] - st[32 + at_row(r, half)] : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] -= st[32 + at_row(r, half)];
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= sc[r];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const at_v8b ph = at_round(sc, 8 * y), sh = at_round(dp, 8 * y);
+            at_v8b pl, sl;
+            if (TWO) {
+                pl = at_rest(sc, 8 * y, ph);
+                sl = at_rest(dp, 8 * y, sh);
+            }
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const at_v8b qt = at_frag(rb[(2 * KS + y * DB + d) * 64]), gt = at_frag(rb[(3 * KS + y * DB + d) * 64]);
+                dv[d] = at_mfma(gt, ph, dv[d]);
+                dk[d] = at_mfma(qt, sh, dk[d]);
+                if (TWO) {
+                    dv[d] = at_mfma(gt, pl, dv[d]);
+                    dk[d] = at_mfma(qt, sl, dk[d]);
+                }
+            }
+        }
+    }
+    bool flagged = false;
+    for (int n = lane; n < blocks; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
+    flagged = __any(flagged);
+    if (key >= s.LK) return;
+    AttnMarks marks = {};
+    if (flagged)
+        for (int n = 0; n < blocks; ++n) {
+            if (!a.flags[rows0 + first + n]) continue;
+            for (int row = (first + n) * 32; row < (first + n) * 32 + 32 && row < s.rows; ++row) {
+                const int i = row / s.G, p = base + i;
+                if (at_sees(s, p, s.window ? p - s.window : -1, key))
+#pragma unroll 1
+                    for (int e = 0; e < 16 * DB; ++e) {
+                        const int d = (e >> 4) * 32 + at_row(e & 15, half);
+                        if (d < s.D) marks.add(e, load_value(a.gsrc, b * a.gb + i * a.gl + (hk * s.G + (row - i * s.G)) * a.gh + d, a.kg, a.fg));
+                    }
+            }
+        }
+    const int64_t at = (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int e = d * 32 + at_row(r, half);
+            if (e >= s.D) continue;
+            store_value(a.dk, at + e, a.kout, a.fout, dk[d][r] * s.scale);
+            float v = dv[d][r];
+            if (flagged) v = marks.apply(16 * d + r, v);
+            store_value(a.dv, at + e, a.kout, a.fout, v);
+        }
+}
+
+}  // namespace pnn
