@@ -1,5 +1,6 @@
 // posit_attention_fwd / posit_attention_bwd: attention with a sliding window and sinks.
 #include "attn_bwd.h"
+#include "attn_token.h"
 
 namespace pnn {
 
@@ -36,6 +37,34 @@ struct Plan {
     int db;
     int64_t nbh, q_bytes, k_bytes;  // of one packed operand
 };
+
+// Few queries on many keys go to the token kernel: it decodes a cache where it reads it and splits its length over workgroups; the
+// prompt kernel reads a packed copy and has a workgroup to 128 rows.
+struct TokenPlan {
+    bool use;
+    int blocks, parts, tiles;  // row blocks of 32, parts of the keys, tiles of 32 keys in a part
+    int64_t bytes;
+};
+
+TokenPlan token_plan(const pnn_attention_desc& d) {
+    TokenPlan t = {};
+    const int64_t g = d.HKV ? d.HQ / d.HKV : 1, rows = d.LQ * g;
+    t.use = rows <= 32 || (rows <= 128 && d.LK >= 4 * rows);
+    if (!t.use) return t;
+    t.blocks = (int)((rows + 31) / 32);
+    int64_t keys = d.LK;
+    if (d.window > 0 && d.window + d.LQ + d.sinks + 64 < keys) keys = d.window + d.LQ + d.sinks + 64;
+    const int64_t all = (keys + 31) / 32 + 1, groups = d.B * d.HKV * t.blocks;
+    // four workgroups to a compute unit, at least four tiles (one to a wave) in a part; short caches stay whole, the second kernel costs more
+    int64_t parts = groups > 0 ? (1024 + groups - 1) / groups : 1;
+    if (parts > all / 4) parts = all / 4;
+    if (parts < 1 || all <= 16) parts = 1;
+    t.tiles = (int)((all + parts - 1) / parts);
+    t.tiles = (t.tiles + 3) / 4 * 4;
+    t.parts = (int)((all + t.tiles - 1) / t.tiles);
+    t.bytes = t.parts > 1 ? groups * t.parts * 32 * (d.D + 2) * 4 : 0;
+    return t;
+}
 
 Plan make_plan(const pnn_attention_desc& d) {
     Plan p;
@@ -93,11 +122,27 @@ void launch_bwd(hipStream_t st, const Plan& p, const AttnBwd& a) {
     }
 }
 
+template <int K>
+void launch_token(hipStream_t st, int db, bool two, const dim3& grid, const AttnToken& a) {
+#define PNN_TOKEN(DB)                                                                                             \
+    if (two) hipLaunchKernelGGL((attn_token_kernel<K, DB, true>), grid, dim3(256), 0, st, a);   \
+    else hipLaunchKernelGGL((attn_token_kernel<K, DB, false>), grid, dim3(256), 0, st, a);
+    switch (db) {
+        case 1: PNN_TOKEN(1) break;
+        case 2: PNN_TOKEN(2) break;
+        case 3: PNN_TOKEN(3) break;
+        default: PNN_TOKEN(4) break;
+    }
+#undef PNN_TOKEN
+}
+
 }  // namespace
 
 extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attention_desc* desc) {
     if (desc_status(desc) || desc->B == 0 || desc->HQ == 0 || desc->D == 0) return 0;
     const Plan p = make_plan(*desc);
+    const TokenPlan t = token_plan(*desc);
+    if (which == 0 && t.use) return (size_t)t.bytes;
     if (which == 0) return (size_t)(p.q_bytes + 2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
     return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4));
 }
@@ -119,6 +164,24 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     discard_stale_hip_error();
     Plan p = make_plan(d);
     p.s.lens = lens;
+    const bool two = fout != PNN_BF16 || (o_copy && fcopy != PNN_BF16);
+    const TokenPlan tp = token_plan(d);
+    if (tp.use) {
+        AttnToken a = {};
+        a.s = p.s; a.q = q; a.k = k; a.v = v;
+        a.qb = d.qb; a.ql = d.ql; a.qh = d.qh; a.kb = d.kb; a.kl = d.kl; a.kh = d.kh; a.vb = d.vb; a.vl = d.vl; a.vh = d.vh;
+        a.kq = kind_of(fq); a.fq = elem_fmt(fq); a.fkv = elem_fmt(fkv);
+        a.o = o; a.copy = o_copy; a.lse = lse; a.ko = kind_of(fout); a.fo = elem_fmt(fout); a.kc = kind_of(o_copy ? fcopy : fout); a.fc = elem_fmt(o_copy ? fcopy : fout);
+        a.tiles = tp.tiles; a.parts = tp.parts; a.part = (float*)workspace;
+        const dim3 grid((unsigned)(tp.blocks * tp.parts), (unsigned)d.HKV, (unsigned)d.B);
+        switch (kind_of(fkv)) {
+            case KIND_POSIT_U8: launch_token<KIND_POSIT_U8>(st, p.db, two, grid, a); break;
+            case KIND_POSIT_U16: launch_token<KIND_POSIT_U16>(st, p.db, two, grid, a); break;
+            default: launch_token<KIND_BF16>(st, p.db, two, grid, a); break;
+        }
+        if (tp.parts > 1) hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)p.s.rows, (unsigned)d.HKV, (unsigned)d.B), dim3(128), 0, st, a);
+        return hip_status(hipGetLastError());
+    }
     uint4* const wq = (uint4*)workspace;
     uint4* const wk = wq + p.q_bytes / 16;
     uint4* const wv = wk + p.k_bytes / 16;
@@ -134,8 +197,8 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     a.ko = kind_of(fout); a.fo = elem_fmt(fout); a.kc = kind_of(o_copy ? fcopy : fout); a.fc = elem_fmt(o_copy ? fcopy : fout);
     a.nbh = (int)p.nbh;
     a.flags = flags; a.vsrc = v; a.vb = d.vb; a.vl = d.vl; a.vh = d.vh; a.kv = kind_of(fkv); a.fv = elem_fmt(fkv);
-    if (fout == PNN_BF16 && (!o_copy || fcopy == PNN_BF16)) launch_fwd<false>(st, p, a);
-    else launch_fwd<true>(st, p, a);
+    if (two) launch_fwd<true>(st, p, a);
+    else launch_fwd<false>(st, p, a);
     return hip_status(hipGetLastError());
 }
 

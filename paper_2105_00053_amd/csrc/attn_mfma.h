@@ -164,6 +164,19 @@ __device__ __forceinline__ at_v8b at_rest(const at_v16f& v, int from, const at_v
     return o;
 }
 
+// The scale of the scores, as what exp2 takes: kept positive, so that the largest score has the largest exponent; its sign goes into q, and where it
+// is zero q does (a NaN in it stays one).
+__device__ __forceinline__ float at_scale(float c) { return c < 0.f ? -c : (c == 0.f ? 1.f : c); }
+__device__ __forceinline__ at_v8b at_scaled(uint4 v, float c) {
+    if (c < 0.f) v = make_uint4(v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u);
+    at_v8b q = at_frag(v);
+    if (c == 0.f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] = (__bf16)((float)q[e] * 0.f);
+    }
+    return q;
+}
+
 // What infinities and NaN that a result's row sees make of it; the packed operand held zeros in their place.
 struct AttnMarks {
     uint32_t pos[2], neg[2], nan[2];  // one bit a result register

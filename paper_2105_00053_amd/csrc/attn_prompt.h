@@ -70,17 +70,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
     {
         const uint4* src = a.q + ((int64_t)bh * s.qblocks + tile * 4 + w) * (KS * 64) + lane;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            uint4 v = src[ks * 64];
-            if (c < 0.f) v = make_uint4(v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u);
-            q[ks] = at_frag(v);
-            if (c == 0.f) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[ks][e] = (__bf16)((float)q[ks][e] * 0.f);
-            }
-        }
+        for (int ks = 0; ks < KS; ++ks) q[ks] = at_scaled(src[ks * 64], c);
     }
-    c = c < 0.f ? -c : (c == 0.f ? 1.f : c);
+    c = at_scale(c);
 
     const uint4* const ksrc = a.k + (int64_t)bh * s.kblocks * (KS * 64);
     const uint4* const vsrc = a.v + (int64_t)bh * s.kblocks * (KS * 64);
