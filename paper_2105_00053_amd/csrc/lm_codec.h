@@ -30,45 +30,52 @@ inline ElemFmt elem_fmt(int f) {
 PNN_HD float f32_of_bits(uint32_t b) { return __builtin_bit_cast(float, b); }
 PNN_HD uint32_t bits_of_f32(float v) { return __builtin_bit_cast(uint32_t, v); }
 
-// Value of a posit of at most 16 bits (exact: at most 13 significant bits, |scale| <= 40).  Regime, exponent and fraction are one
-// string; with the regime's k taken off, what is left is exponent and fraction as binary32 has them, shifted.
+// A posit's magnitude pattern and its value are tied by one integer:  T = k 2^(23+es) + (exponent and fraction, 23 + es bits)  is the
+// binary32 word of the value less that of 1.  Two facts make both directions short:
+//  - negating the n-1 bits of the pattern negates T (regime ones become zeros, what follows its complement), so only values
+//    below 1 need to be handled: their regime is a run of zeros and its terminating one;
+//  - that is how an integer looks to the conversion between integers and binary32: converting the pattern to binary32
+//    counts the run and puts exponent and fraction at the top of the significand, adding 2^23 to a binary32 puts a significand behind
+//    a run of zeros and rounds it, nearest with ties to even.
+
+// Value of a posit of at most 16 bits, exact (at most 13 significant bits, |scale| <= 40); NaR gives NaN.
 PNN_HD float posit_value(uint32_t p, ElemFmt f) {
     const int32_t u = (int32_t)(p << (32 - f.n));               // sign on top; zeros below the pattern
-    const uint32_t a = (uint32_t)(u < 0 ? 0 - (uint32_t)u : (uint32_t)u);
-    const uint32_t x = a << 1;                                   // regime on top
-    const uint32_t ones = (uint32_t)((int32_t)x >> 31);
-    const uint32_t run = (uint32_t)clz32(x ^ ones);              // run length (the bit behind the pattern ends it at the latest)
-    const uint32_t k = (run ^ ~ones) + 1u + 2u * ones;           // run - 1 or -run
-    const uint32_t rest = (x << (run & 31u)) << 1;               // exponent, then fraction
-    const uint32_t mag = ((127u + (k << f.es)) << 23) + (rest >> (9 - f.es));
-    const uint32_t v = mag | ((uint32_t)u & 0x80000000u);
-    return f32_of_bits((uint32_t)u == 0x80000000u ? 0x7FC00000u : (u == 0 ? 0u : v));
+    const uint32_t x = (uint32_t)(u < 0 ? 0 - (uint32_t)u : (uint32_t)u) << 1;  // regime on top
+    const uint32_t s = (uint32_t)((int32_t)x >> 31);            // 1 and above
+    const uint32_t y = (x ^ s) - s;
+    const uint32_t t = (bits_of_f32((float)y) << f.es) - (158u << (23 + f.es));
+    const uint32_t mag = (t ^ s) + ((127u << 23) - s);
+    const uint32_t v = (mag & 0x7FFFFFFFu) | ((uint32_t)u & 0x80000000u);
+    return f32_of_bits(y == 0u ? (uint32_t)(u >> 9) : v);        // zero, or a quiet NaN
 }
 
 // Nearest posit of at most 16 bits, ties to the even pattern, never zero or NaR for a finite nonzero value; NaN and infinities
-// give NaR.  The string regime | exponent | fraction comes from an arithmetic right shift of "10" in front of exponent and fraction (for
-// a negative k everything complemented); fraction bits that the cut cannot reach are folded into one that no shift pushes out.
+// give NaR.  `value` receives what the pattern stands for.
+template <bool VALUE>
+PNN_HD uint32_t posit_nearest(float v, ElemFmt f, float& value) {
+    const uint32_t bits = bits_of_f32(v), ah = bits & 0x7FFFFFFFu;
+    const int32_t range = (int32_t)((uint32_t)((f.n - 2) << f.es) << 23), raw = (int32_t)(ah - (127u << 23));
+    const int32_t t = raw < -range ? -range : (raw > range ? range : raw);
+    const int32_t below = t < 0 ? t : -t;
+    // es bits leave the significand; they stay as "not zero" in its last ones, far below any cut
+    const uint32_t g = (uint32_t)(below >> f.es) | ((uint32_t)below & ((1u << f.es) - 1u));
+    const float cut = f32_of_bits(g + ((uint32_t)(127 + f.n - 2) << 23)) + 8388608.f;
+    const uint32_t st = (uint32_t)(t >> 31), sb = (uint32_t)((int32_t)bits >> 31);
+    const uint32_t m = ~(st ^ sb);                                // negate: for a value of 1 and above, and for a negative one
+    const uint32_t p = ((bits_of_f32(cut) ^ m) - m + (~st & (1u << (f.n - 1)))) & ((1u << f.n) - 1u);
+    const bool zero = ah == 0u, nar = ah >= 0x7F800000u;
+    if (VALUE) {
+        const uint32_t r = (bits_of_f32(cut - 8388608.f) - ((uint32_t)(127 + f.n - 2) << 23)) << f.es;
+        const uint32_t mag = (r ^ ~st) - ~st + (127u << 23);
+        const uint32_t w = (mag & 0x7FFFFFFFu) | (bits & 0x80000000u);
+        value = f32_of_bits(zero ? 0u : (nar ? 0x7FC00000u : w));
+    }
+    return zero ? 0u : (nar ? 1u << (f.n - 1) : p);
+}
 PNN_HD uint32_t posit_nearest(float v, ElemFmt f) {
-    const uint32_t bits = bits_of_f32(v);
-    const uint32_t ah0 = bits & 0x7FFFFFFFu;
-    const uint32_t range = (uint32_t)((f.n - 2) << f.es) << 23, one = 127u << 23;
-    const uint32_t low = ah0 < one - range ? one - range : ah0;
-    const uint32_t h = (low > one + range ? one + range : low) - one;
-    const int k = (int32_t)h >> (23 + f.es);
-    const uint32_t sg = (uint32_t)(k >> 31);
-    const uint32_t kk = (uint32_t)k ^ sg;
-    uint32_t tail = h << (9 - f.es);
-    const uint32_t reach = 1u << f.n;                            // bits of the tail below this one lie behind every cut
-    tail |= (tail & (reach - 1u)) ? reach : 0u;
-    const uint32_t w = 0x80000000u | ((tail ^ sg) >> 2);
-    const uint32_t x = (uint32_t)((int32_t)w >> kk) ^ sg;
-    const int cut = 33 - f.n;
-    const uint32_t lsb = (x >> cut) & 1u;
-    const uint32_t body = (x + ((1u << (cut - 1)) - 1u) + lsb) >> cut;
-    const uint32_t sm = (uint32_t)((int32_t)bits >> 31);
-    const uint32_t mask = (1u << f.n) - 1u;
-    const uint32_t p = ((body ^ sm) - sm) & mask;
-    return ah0 == 0u ? 0u : (ah0 >= 0x7F800000u ? 1u << (f.n - 1) : p);
+    float none;
+    return posit_nearest<false>(v, f, none);
 }
 
 // ---- in memory ----
@@ -110,33 +117,124 @@ PNN_HD void store_value(void* p, int64_t i, int kind, ElemFmt f, float v) {
     }
 }
 
-// CALL sees `K`, the kind as a constant
-#define PNN_DISPATCH_KIND(kind, CALL)                               \
-    switch (kind) {                                                  \
-        case KIND_POSIT_U8: { constexpr int K = KIND_POSIT_U8; CALL; } break;   \
-        case KIND_POSIT_U16: { constexpr int K = KIND_POSIT_U16; CALL; } break; \
-        case KIND_BF16: { constexpr int K = KIND_BF16; CALL; } break;           \
-        default: { constexpr int K = KIND_F32; CALL; } break;                   \
-    }
+// ---- eight elements in a row, of a kind known at run time (uniform: the branches are the wave's) ----
+// As they lie in memory; alignment is the element type's (wide loads and stores take any address here).
+struct Raw8 {
+    uint32_t w[8];
+};
 
-// ---- sums over a workgroup, in a fixed order ----
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ void load8(Raw8& r, const void* p, int64_t i, int kind, int left) {
+    if (left >= 8) {
+        if (kind == KIND_POSIT_U8) __builtin_memcpy(r.w, (const uint8_t*)p + i, 8);
+        else if (kind == KIND_F32) __builtin_memcpy(r.w, (const uint8_t*)p + 4 * i, 32);
+        else __builtin_memcpy(r.w, (const uint8_t*)p + 2 * i, 16);
+        return;
+    }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
-    return v;
+    for (int e = 0; e < 8; ++e) r.w[e] = 0;
+    if (kind == KIND_POSIT_U8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) r.w[e / 4] |= (uint32_t)((const uint8_t*)p)[i + e] << (8 * (e & 3));
+    } else if (kind == KIND_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) r.w[e] = ((const uint32_t*)p)[i + e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) r.w[e / 2] |= (uint32_t)((const uint16_t*)p)[i + e] << (16 * (e & 1));
+    }
+}
+
+__device__ __forceinline__ void values8(float (&v)[8], const Raw8& r, int kind, ElemFmt f) {
+    if (kind == KIND_POSIT_U8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = posit_value((r.w[e / 4] >> (8 * (e & 3))) & 0xFFu, f);
+    } else if (kind == KIND_POSIT_U16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = posit_value(e & 1 ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xFFFFu, f);
+    } else if (kind == KIND_BF16) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = f32_of_bits(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = f32_of_bits(r.w[e]);
+    }
+}
+
+// Rounds in place where VALUE (v receives what is stored).
+template <bool VALUE>
+__device__ __forceinline__ void raw8(Raw8& r, float (&v)[8], int kind, ElemFmt f) {
+    if (kind == KIND_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w[e] = bits_of_f32(v[e]);
+    } else if (kind == KIND_BF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            r.w[e] = raw_of<KIND_BF16>(v[2 * e], f) | raw_of<KIND_BF16>(v[2 * e + 1], f) << 16;
+            if (VALUE) {
+                v[2 * e] = f32_of_bits(r.w[e] << 16);
+                v[2 * e + 1] = f32_of_bits(r.w[e] & 0xFFFF0000u);
+            }
+        }
+    } else {
+        uint32_t q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float back = 0.f;
+            q[e] = posit_nearest<VALUE>(v[e], f, back);
+            if (VALUE) v[e] = back;
+        }
+        if (kind == KIND_POSIT_U8) {
+            r.w[0] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+            r.w[1] = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.w[e] = q[2 * e] | q[2 * e + 1] << 16;
+        }
+    }
+}
+
+__device__ __forceinline__ void store8(void* p, int64_t i, const Raw8& r, int kind, int left) {
+    if (left >= 8) {
+        if (kind == KIND_POSIT_U8) __builtin_memcpy((uint8_t*)p + i, r.w, 8);
+        else if (kind == KIND_F32) __builtin_memcpy((uint8_t*)p + 4 * i, r.w, 32);
+        else __builtin_memcpy((uint8_t*)p + 2 * i, r.w, 16);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (e >= left) continue;
+        if (kind == KIND_POSIT_U8) ((uint8_t*)p)[i + e] = (uint8_t)(r.w[e / 4] >> (8 * (e & 3)));
+        else if (kind == KIND_F32) ((uint32_t*)p)[i + e] = r.w[e];
+        else ((uint16_t*)p)[i + e] = (uint16_t)(r.w[e / 2] >> (16 * (e & 1)));
+    }
+}
+
+// ---- sums and maxima over a wave, in a fixed order, in every lane ----
+// Through the vector unit's own lane shifts (a shuffle through LDS takes ten times as long); the total arrives in lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_shift(uint32_t v, uint32_t none) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#define PNN_STEP(CTRL, ROWS) v += f32_of_bits(lane_shift<CTRL, ROWS>(bits_of_f32(v), 0u));
+    PNN_STEP(0x111, 0xF) PNN_STEP(0x112, 0xF) PNN_STEP(0x114, 0xF) PNN_STEP(0x118, 0xF) PNN_STEP(0x142, 0xA) PNN_STEP(0x143, 0xC)
+#undef PNN_STEP
+    return f32_of_bits((uint32_t)__builtin_amdgcn_readlane((int)bits_of_f32(v), 63));
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor(v, m, 64));
-    return v;
+#define PNN_STEP(CTRL, ROWS) v = fmaxf(v, f32_of_bits(lane_shift<CTRL, ROWS>(bits_of_f32(v), 0xFF800000u)));
+    PNN_STEP(0x111, 0xF) PNN_STEP(0x112, 0xF) PNN_STEP(0x114, 0xF) PNN_STEP(0x118, 0xF) PNN_STEP(0x142, 0xA) PNN_STEP(0x143, 0xC)
+#undef PNN_STEP
+    return f32_of_bits((uint32_t)__builtin_amdgcn_readlane((int)bits_of_f32(v), 63));
 }
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, m, 64);
-        v = v > o ? v : o;
-    }
-    return v;
+#define PNN_STEP(CTRL, ROWS) { const uint32_t o = lane_shift<CTRL, ROWS>(v, 0u); v = v > o ? v : o; }
+    PNN_STEP(0x111, 0xF) PNN_STEP(0x112, 0xF) PNN_STEP(0x114, 0xF) PNN_STEP(0x118, 0xF) PNN_STEP(0x142, 0xA) PNN_STEP(0x143, 0xC)
+#undef PNN_STEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 }  // namespace pnn
