@@ -117,6 +117,15 @@ PNN_HD void store_value(void* p, int64_t i, int kind, ElemFmt f, float v) {
     }
 }
 
+// CALL sees `K`, the kind as a constant
+#define PNN_DISPATCH_KIND(kind, CALL)                               \
+    switch (kind) {                                                  \
+        case KIND_POSIT_U8: { constexpr int K = KIND_POSIT_U8; CALL; } break;   \
+        case KIND_POSIT_U16: { constexpr int K = KIND_POSIT_U16; CALL; } break; \
+        case KIND_BF16: { constexpr int K = KIND_BF16; CALL; } break;           \
+        default: { constexpr int K = KIND_F32; CALL; } break;                   \
+    }
+
 // ---- eight elements in a row, of a kind known at run time (uniform: the branches are the wave's) ----
 // As they lie in memory; alignment is the element type's (wide loads and stores take any address here).
 struct Raw8 {
