@@ -41,97 +41,117 @@ __device__ __forceinline__ uint32_t block_max_u32(uint32_t v, uint32_t* part) {
     return m;
 }
 
-// Rows that fit the registers of T threads, 8 C elements to a thread: read once, with the next row's loads in flight, written once.
-// The weights are decoded once for all rows of a workgroup.
-template <int T, int C>
-__global__ __launch_bounds__(256) void rmsnorm_fwd_rows_kernel(NormFwd a) {
-    __shared__ float part[2][4];
-    __shared__ uint32_t partu[2][4];
-    const int t = threadIdx.x, tr = t % T, cols = (int)a.cols;
-    const bool add = a.res != nullptr;
-    float w[C][8];
+// Values of 8-bit posits by look-up: 16 copies of each in LDS, so that the lanes of a wave meet few conflicts.  Pays where a workgroup
+// has rows enough (a look-up takes 3 vector instructions, decoding 17; building the table as long as two rows).
+constexpr int NORM_COPIES = 16, NORM_TABLE_ROWS = 4;
+__device__ __forceinline__ void norm_table(uint32_t* table, ElemFmt f) {
+    for (int e = threadIdx.x; e < 256 * NORM_COPIES / 4; e += blockDim.x) {
+        const uint32_t v = bits_of_f32(posit_value(e / (NORM_COPIES / 4), f));
+        ((uint4*)table)[e] = make_uint4(v, v, v, v);
+    }
+    __syncthreads();
+}
+template <int K>
+__device__ __forceinline__ void norm_values(float (&v)[8], const Raw8& r, ElemFmt f, const uint32_t* table) {
+    if (K == KIND_POSIT_U8 && table) {
+        const uint32_t* mine = table + (threadIdx.x & (NORM_COPIES - 1));
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        Raw8 r;
-        load8(r, a.w, (c * T + tr) * 8, a.kw, cols - (c * T + tr) * 8);
-        values8(w[c], r, a.kw, a.fw);
+        for (int e = 0; e < 8; ++e) v[e] = f32_of_bits(mine[((r.w[e / 4] >> (8 * (e & 3))) & 0xFFu) * NORM_COPIES]);
+    } else {
+        values8(v, r, K, f);
+    }
+}
+
+// Sum (and maximum) over the T threads of a row; `slot` alternates, so that one barrier is enough.
+__device__ __forceinline__ void norm_reduce(int T, float* part, uint32_t* partu, int slot, float& s, uint32_t& top, bool maximum) {
+    s = wave_sum(s);
+    if (maximum) top = wave_max_u32(top);
+    if (T == 64) return;
+    const int t = threadIdx.x, waves = T / 64, first = t / T * waves;
+    if ((t & 63) == 0) {
+        part[slot * 16 + (t >> 6)] = s;
+        if (maximum) partu[slot * 16 + (t >> 6)] = top;
+    }
+    __syncthreads();
+    s = 0.f;
+    for (int i = 0; i < waves; ++i) s += part[slot * 16 + first + i];
+    if (maximum) {
+        top = 0;
+        for (int i = 0; i < waves; ++i) top = partu[slot * 16 + first + i] > top ? partu[slot * 16 + first + i] : top;
+    }
+}
+
+// Rows of up to 8192 elements, 8 to a thread: read once, with the next row's loads in flight, written once.  T threads (a power of two
+// of waves) to a row; the weights are decoded once for all rows of a workgroup.  KR < 0: no residual.
+template <int KX, int KR>
+__global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T) {
+    __shared__ float part[32];
+    __shared__ uint32_t partu[32];
+    __shared__ uint32_t table_of[KX == KIND_POSIT_U8 ? 256 * NORM_COPIES : 1];
+    const int t = threadIdx.x, group = t / T, j = (t - group * T) * 8, groups = blockDim.x / T, cols = (int)a.cols;
+    const bool scaled = a.scale != nullptr;
+    Raw8 x, res;
+    auto load = [&](int64_t r) {
+        const int left = r < a.rows ? cols - j : 0;
+        load8(x, a.x, r * a.ldx + j, KX, left);
+        if (KR >= 0) load8(res, a.res, r * a.ldr + j, KR, left);
+    };
+    const int64_t step = (int64_t)gridDim.x * groups;
+    int64_t r = (int64_t)blockIdx.x * groups + group;
+    load(r);
+    float w[8];
+    {
+        Raw8 raw;
+        load8(raw, a.w, j, a.kw, cols - j);
+        values8(w, raw, a.kw, a.fw);
+    }
+    const uint32_t* table = nullptr;
+    if (KX == KIND_POSIT_U8 && a.rows >= NORM_TABLE_ROWS * step) {
+        norm_table(table_of, a.fx);
+        table = table_of;
     }
     const float inv = 1.f / (float)cols;
-    Raw8 x[C], res[C];
-    auto load = [&](int64_t r) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = (c * T + tr) * 8, left = r < a.rows ? cols - j : 0;
-            load8(x[c], a.x, r * a.ldx + j, a.kx, left);
-            if (add) load8(res[c], a.res, r * a.ldr + j, a.kr, left);
-        }
-    };
-    const int64_t step = (int64_t)gridDim.x * (256 / T);
-    int64_t r = (int64_t)blockIdx.x * (256 / T) + t / T;
-    load(r);
+    int slot = 0;
     // a workgroup's rows end together, so that its threads meet at the barriers
-    for (int64_t r0 = (int64_t)blockIdx.x * (256 / T), n = 0; r0 < a.rows; r0 += step, r += step, ++n) {
-        float h[C][8];
+    for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < a.rows; r0 += step, r += step, slot ^= 1) {
+        float h[8];
+        norm_values<KX>(h, x, a.fx, table);
+        if (KR >= 0) {
+            float v[8];
+            values8(v, res, KR, a.fr);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] += v[e];
+            load(r + step);
+            Raw8 out;
+            raw8<true>(out, h, KR, a.fr);
+            if (r < a.rows) store8(a.res_out, r * a.ldo + j, out, KR, cols - j);
+        } else {
+            load(r + step);
+        }
+        uint32_t top = 0;
         float ss = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            values8(h[c], x[c], a.kx, a.fx);
-            if (add) {
-                float v[8];
-                values8(v, res[c], a.kr, a.fr);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[c][e] += v[e];
-                const int j = (c * T + tr) * 8;
-                Raw8 out;
-                raw8<true>(out, h[c], a.kr, a.fr);
-                if (r < a.rows) store8(a.res_out, r * a.ldo + j, out, a.kr, cols - j);
-            }
+        for (int e = 0; e < 8; ++e) {
+            ss = fmaf(h[e], h[e], ss);
+            h[e] *= w[e];
+            const uint32_t m = bits_of_f32(h[e]) & 0x7FFFFFFFu;
+            top = m > top ? m : top;
         }
-        load(r + step);
-        uint32_t top = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ss = fmaf(h[c][e], h[c][e], ss);
-                h[c][e] *= w[c][e];
-                if (a.scale) {
-                    const uint32_t m = bits_of_f32(h[c][e]) & 0x7FFFFFFFu;
-                    top = m > top ? m : top;
-                }
-            }
-        ss = wave_sum(ss);
-        if (a.scale) top = wave_max_u32(top);
-        if (T > 64) {
-            if ((t & 63) == 0) {
-                part[n & 1][t >> 6] = ss;
-                partu[n & 1][t >> 6] = top;
-            }
-            __syncthreads();
-            const float* p = part[n & 1];
-            const uint32_t* u = partu[n & 1];
-            ss = (p[0] + p[1]) + (p[2] + p[3]);
-            const uint32_t u0 = u[0] > u[1] ? u[0] : u[1], u1 = u[2] > u[3] ? u[2] : u[3];
-            top = u0 > u1 ? u0 : u1;
-        }
+        norm_reduce(T, part, partu, slot, ss, top, scaled);
         if (r >= a.rows) continue;
         const float rstd = 1.f / sqrtf(ss * inv + a.eps);
         float up = rstd;
-        if (a.scale) {
+        if (scaled) {
             float down;
             const bool bad = norm_scale(top, up, down);
-            if (tr == 0) a.scale[r] = bad ? f32_of_bits(0x7FC00000u) : rstd * down;
+            if (j == 0) a.scale[r] = bad ? f32_of_bits(0x7FC00000u) : rstd * down;
         }
-        if (a.rstd && tr == 0) a.rstd[r] = rstd;
+        if (a.rstd && j == 0) a.rstd[r] = rstd;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = (c * T + tr) * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) h[c][e] *= up;
-            Raw8 out;
-            raw8<false>(out, h[c], a.ky, a.fy);
-            store8(a.y, r * a.ldy + j, out, a.ky, cols - j);
-        }
+        for (int e = 0; e < 8; ++e) h[e] *= up;
+        Raw8 out;
+        raw8<false>(out, h, a.ky, a.fy);
+        store8(a.y, r * a.ldy + j, out, a.ky, cols - j);
     }
 }
 
@@ -183,116 +203,110 @@ struct NormBwd {
 };
 
 // As the forward kernel for rows; each thread also sums its columns of dw over the workgroup's rows, and leaves the sums for
-// rmsnorm_dw_join_kernel (one row of `part` to a workgroup; its waves are joined in LDS where a row is a wave's).
-template <int T, int C>
-__global__ __launch_bounds__(256) void rmsnorm_bwd_rows_kernel(NormBwd a) {
-    __shared__ float sums[2][4];
-    __shared__ float join[T == 64 ? 3 * C * 512 : 1];
-    const int t = threadIdx.x, tr = t % T, cols = (int)a.cols;
-    float w[C][8], dw[C][8];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        Raw8 r;
-        load8(r, a.w, (c * T + tr) * 8, a.kw, cols - (c * T + tr) * 8);
-        values8(w[c], r, a.kw, a.fw);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dw[c][e] = 0.f;
-    }
-    const float inv = 1.f / (float)cols;
-    Raw8 dy[C], hr[C], dres[C];
+// rmsnorm_dw_join_kernel (one row of `part` to a workgroup, whose rows in parallel are joined in LDS).  KR < 0: no gradient past the norm; KR other than
+// KD: its kind is a.kr.
+template <int KD, int KH, int KR>
+__global__ __launch_bounds__(1024) void rmsnorm_bwd_rows_kernel(NormBwd a, int T) {
+    __shared__ float part[32];
+    __shared__ float join[3 * 512];
+    __shared__ uint32_t table_of[KD == KIND_POSIT_U8 ? 256 * NORM_COPIES : 1];
+    const int t = threadIdx.x, group = t / T, tr = t - group * T, j = tr * 8, groups = blockDim.x / T, cols = (int)a.cols;
+    const int kr = KR == KD ? KD : a.kr;
+    Raw8 dy, hr, dres;
     float rs = 0.f;
     auto load = [&](int64_t r) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = (c * T + tr) * 8, left = r < a.rows ? cols - j : 0;
-            load8(dy[c], a.dy, r * a.lddy + j, a.kd, left);
-            load8(hr[c], a.h, r * a.ldh + j, a.kh, left);
-            if (a.dres) load8(dres[c], a.dres, r * a.lddr + j, a.kr, left);
-        }
+        const int left = r < a.rows ? cols - j : 0;
+        load8(dy, a.dy, r * a.lddy + j, KD, left);
+        load8(hr, a.h, r * a.ldh + j, KH, left);
+        if (KR >= 0) load8(dres, a.dres, r * a.lddr + j, kr, left);
         rs = r < a.rows ? a.rstd[r] : 0.f;
     };
-    const int64_t step = (int64_t)gridDim.x * (256 / T);
-    int64_t r = (int64_t)blockIdx.x * (256 / T) + t / T;
+    const int64_t step = (int64_t)gridDim.x * groups;
+    int64_t r = (int64_t)blockIdx.x * groups + group;
     load(r);
-    for (int64_t r0 = (int64_t)blockIdx.x * (256 / T), n = 0; r0 < a.rows; r0 += step, r += step, ++n) {
-        float g[C][8], h[C][8], past[C][8];
-        float s = 0.f;
+    float w[8], dw[8];
+    {
+        Raw8 raw;
+        load8(raw, a.w, j, a.kw, cols - j);
+        values8(w, raw, a.kw, a.fw);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[e] = 0.f;
+    const uint32_t* table = nullptr;
+    if (KD == KIND_POSIT_U8 && a.rows >= NORM_TABLE_ROWS * step) {
+        norm_table(table_of, a.fd);
+        table = table_of;
+    }
+    const float inv = 1.f / (float)cols;
+    int slot = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < a.rows; r0 += step, r += step, slot ^= 1) {
+        float g[8], h[8], past[8];
         const float rstd = rs;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            values8(g[c], dy[c], a.kd, a.fd);
-            values8(h[c], hr[c], a.kh, a.fh);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) past[c][e] = 0.f;
-            if (a.dres) values8(past[c], dres[c], a.kr, a.fr);
-        }
-        load(r + step);
         const bool live = r < a.rows;
+        norm_values<KD>(g, dy, a.fd, table);
+        values8(h, hr, KH, a.fh);
+        if (KR >= 0) values8(past, dres, kr, a.fr);
+        load(r + step);
+        float s = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (live) dw[c][e] = fmaf(g[c][e] * rstd, h[c][e], dw[c][e]);
-                g[c][e] *= w[c][e];
-                s = fmaf(g[c][e], h[c][e], s);
-            }
-        s = wave_sum(s);
-        if (T > 64) {
-            if ((t & 63) == 0) sums[n & 1][t >> 6] = s;
-            __syncthreads();
-            const float* p = sums[n & 1];
-            s = (p[0] + p[1]) + (p[2] + p[3]);
+        for (int e = 0; e < 8; ++e) {
+            dw[e] = live ? fmaf(g[e] * rstd, h[e], dw[e]) : dw[e];
+            g[e] *= w[e];
+            s = fmaf(g[e], h[e], s);
         }
+        uint32_t none = 0;
+        norm_reduce(T, part, nullptr, slot, s, none, false);
         if (!live) continue;
         const float k = s * inv * rstd * rstd * rstd;
+        float v[8];
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int j = (c * T + tr) * 8;
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = rstd * g[c][e] - k * h[c][e] + past[c][e];
-            Raw8 out;
-            raw8<false>(out, v, a.kx, a.fx);
-            store8(a.dx, r * a.lddx + j, out, a.kx, cols - j);
+        for (int e = 0; e < 8; ++e) {
+            v[e] = rstd * g[e] - k * h[e];
+            if (KR >= 0) v[e] += past[e];
         }
+        Raw8 out;
+        raw8<false>(out, v, a.kx, a.fx);
+        store8(a.dx, r * a.lddx + j, out, a.kx, cols - j);
     }
     if (!a.dw) return;
-    if (T == 64) {
-        const int wave = t >> 6;
+    // groups of threads only where a workgroup is 256 threads: 4 of 64 or 2 of 128
+    if (groups > 1) {
+        if (group > 0) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (wave > 0) join[((wave - 1) * C * 8 + c * 8 + e) * 64 + tr] = dw[c][e];
+            for (int e = 0; e < 8; ++e) join[((group - 1) * 8 + e) * T + tr] = dw[e];
+        }
         __syncthreads();
-        if (wave > 0) return;
+        if (group > 0) return;
+        for (int x = 0; x < groups - 1; ++x)
 #pragma unroll
-        for (int x = 0; x < 3; ++x)
-#pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dw[c][e] += join[(x * C * 8 + c * 8 + e) * 64 + tr];
+            for (int e = 0; e < 8; ++e) dw[e] += join[(x * 8 + e) * T + tr];
     }
-    float* const out = a.part + (int64_t)blockIdx.x * a.cols;
+    float* const out = a.part + (int64_t)blockIdx.x * a.cols + j;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if ((c * T + tr) * 8 + e < cols) out[(c * T + tr) * 8 + e] = dw[c][e];
+    for (int e = 0; e < 8; ++e)
+        if (j + e < cols) out[e] = dw[e];
 }
 
-// Columns of the partial sums: 16 columns to a workgroup, 16 threads to a column, in a fixed order.
-__global__ __launch_bounds__(256) void rmsnorm_dw_join_kernel(const float* part, int64_t groups, int64_t cols, void* dw, int kind, ElemFmt f) {
-    __shared__ float sums[16][17];
-    const int c = threadIdx.x & 15, y = threadIdx.x >> 4;
-    const int64_t j = (int64_t)blockIdx.x * 16 + c;
+// Columns of the partial sums: 32 columns to a workgroup, 32 threads to a column, in a fixed order.
+__global__ __launch_bounds__(1024) void rmsnorm_dw_join_kernel(const float* part, int groups, int64_t cols, void* dw, int kind, ElemFmt f) {
+    __shared__ float sums[32][33];
+    const int c = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t j = (int64_t)blockIdx.x * 32 + c;
     float s = 0.f;
-    if (j < cols)
-        for (int64_t g = y; g < groups; g += 16) s += part[g * cols + j];
+    if (j < cols) {
+        int g = y;
+        for (; g + 96 < groups; g += 128) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = part[(int64_t)(g + 32 * i) * cols + j];
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; g < groups; g += 32) s += part[(int64_t)g * cols + j];
+    }
     sums[y][c] = s;
     __syncthreads();
     if (y == 0 && j < cols) {
-        for (int k = 1; k < 16; ++k) s += sums[k][c];
+        for (int k = 1; k < 32; ++k) s += sums[k][c];
         store_value(dw, j, kind, f, s);
     }
 }
@@ -342,22 +356,44 @@ __global__ __launch_bounds__(256) void scale_rows_kernel(const void* x, int64_t 
     store8(y, r * ldy + j, raw, ky, left);
 }
 
-// Threads to a row and vectors of 8 to a thread, by the row's length: a wave as long as a row is 16 elements a thread, else a
-// workgroup.  BEFORE runs where one of them applies, with the grid's size in `groups`.
-#define PNN_NORM_LAUNCH(KERNEL, T, C, BEFORE)                                                         \
-    {                                                                                                  \
-        const int64_t want = (rows + 256 / T - 1) / (256 / T);                                          \
-        const unsigned groups = (unsigned)(want < NORM_GROUPS ? want : NORM_GROUPS);                      \
-        BEFORE;                                                                                          \
-        hipLaunchKernelGGL((KERNEL<T, C>), dim3(groups), dim3(256), 0, st, a);                             \
+// Threads to a row, threads and number of workgroups.  Rows beyond 8 elements a thread of the largest workgroup have kernels of their own.
+struct NormPlan {
+    bool rows;
+    int T, threads;
+    unsigned groups;
+};
+inline NormPlan norm_plan(int64_t rows, int64_t cols) {
+    NormPlan p = {cols <= 8192, 64, 256, 0};
+    while (p.T * 8 < cols && p.T < 1024) p.T *= 2;
+    if (p.threads < p.T) p.threads = p.T;
+    // as many workgroups as the chip holds, 2048 threads to a compute unit; each walks over rows
+    const int64_t want = (rows + p.threads / p.T - 1) / (p.threads / p.T), most = 256 * 2048 / p.threads;
+    p.groups = (unsigned)(want < most ? want : most);
+    return p;
+}
+
+template <int KX>
+void launch_fwd_rows(hipStream_t st, const NormPlan& p, const NormFwd& a) {
+    const dim3 g(p.groups), b(p.threads);
+    if (!a.res) {
+        hipLaunchKernelGGL((rmsnorm_fwd_rows_kernel<KX, -1>), g, b, 0, st, a, p.T);
+        return;
     }
-#define PNN_NORM_ROWS(cols, KERNEL, BEFORE)                          \
-    if (cols <= 512) PNN_NORM_LAUNCH(KERNEL, 64, 1, BEFORE)           \
-    else if (cols <= 1024) PNN_NORM_LAUNCH(KERNEL, 64, 2, BEFORE)      \
-    else if (cols <= 2048) PNN_NORM_LAUNCH(KERNEL, 256, 1, BEFORE)      \
-    else if (cols <= 4096) PNN_NORM_LAUNCH(KERNEL, 256, 2, BEFORE)       \
-    else if (cols <= 8192) PNN_NORM_LAUNCH(KERNEL, 256, 4, BEFORE)
-constexpr int64_t NORM_GROUPS = 1024;
+    PNN_DISPATCH_KIND(a.kr, hipLaunchKernelGGL((rmsnorm_fwd_rows_kernel<KX, K>), g, b, 0, st, a, p.T))
+}
+
+template <int KD, int KH>
+void launch_bwd_rows(hipStream_t st, const NormPlan& p, const NormBwd& a) {
+    const dim3 g(p.groups), b(p.threads);
+    constexpr int OTHER = KD == KIND_F32 ? KIND_BF16 : KIND_F32;  // any kind that is not KD
+    if (!a.dres) hipLaunchKernelGGL((rmsnorm_bwd_rows_kernel<KD, KH, -1>), g, b, 0, st, a, p.T);
+    else if (a.kr == KD) hipLaunchKernelGGL((rmsnorm_bwd_rows_kernel<KD, KH, KD>), g, b, 0, st, a, p.T);
+    else hipLaunchKernelGGL((rmsnorm_bwd_rows_kernel<KD, KH, OTHER>), g, b, 0, st, a, p.T);
+}
+template <int KD>
+void launch_bwd_rows_of(hipStream_t st, const NormPlan& p, const NormBwd& a) {
+    PNN_DISPATCH_KIND(a.kh, (launch_bwd_rows<KD, K>(st, p, a)))
+}
 
 }  // namespace pnn
 
@@ -375,15 +411,16 @@ extern "C" int posit_rmsnorm_fwd(void* stream, int fx, int fres, int fw, int fy,
     NormFwd a = {x, res, w, res_out, y, scale, rstd, rows, cols, ldx, ldr, ldo, ldy, eps, kind_of(fx), res ? kind_of(fres) : 0, kind_of(fw), kind_of(fy),
                  elem_fmt(fx), elem_fmt(res ? fres : fx), elem_fmt(fw), elem_fmt(fy)};
     hipStream_t st = (hipStream_t)stream;
-    PNN_NORM_ROWS(cols, rmsnorm_fwd_rows_kernel, (void)0)
-    else hipLaunchKernelGGL(rmsnorm_fwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+    const NormPlan p = norm_plan(rows, cols);
+    if (p.rows) {
+        PNN_DISPATCH_KIND(a.kx, launch_fwd_rows<K>(st, p, a))
+    } else hipLaunchKernelGGL(rmsnorm_fwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
     return hip_status(hipGetLastError());
 }
 
 extern "C" size_t posit_rmsnorm_bwd_workspace(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0 || cols > 8192) return 0;
-    const int64_t per = cols <= 1024 ? 4 : 1, want = (rows + per - 1) / per;
-    return (size_t)((want < NORM_GROUPS ? want : NORM_GROUPS) * cols * 4);
+    return (size_t)norm_plan(rows, cols).groups * (size_t)cols * 4;
 }
 
 extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres, int fdx, int fdw, int64_t rows, int64_t cols, const void* dy, int64_t lddy,
@@ -402,13 +439,14 @@ extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres
     NormBwd a = {dy, h, w, dres, rstd, dx, dw, rows, cols, lddy, ldh, lddr, lddx, kind_of(fd), kind_of(fh), kind_of(fw), kind_of(dres ? fdres : fd), kind_of(fdx),
                  kind_of(dw ? fdw : fd), elem_fmt(fd), elem_fmt(fh), elem_fmt(fw), elem_fmt(dres ? fdres : fd), elem_fmt(fdx), elem_fmt(dw ? fdw : fd), (float*)workspace};
     hipStream_t st = (hipStream_t)stream;
-    unsigned used = 0;
-    PNN_NORM_ROWS(cols, rmsnorm_bwd_rows_kernel, used = groups)
-    else {
+    const NormPlan p = norm_plan(rows, cols);
+    if (p.rows) {
+        PNN_DISPATCH_KIND(a.kd, launch_bwd_rows_of<K>(st, p, a))
+        if (dw) hipLaunchKernelGGL(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, st, a.part, (int)p.groups, cols, dw, a.kdw, a.fdw);
+    } else {
         hipLaunchKernelGGL(rmsnorm_bwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
         if (dw) hipLaunchKernelGGL(rmsnorm_dw_kernel, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, st, a);
     }
-    if (dw && used) hipLaunchKernelGGL(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + 15) / 16)), dim3(256), 0, st, a.part, (int64_t)used, cols, dw, a.kdw, a.fdw);
     return hip_status(hipGetLastError());
 }
 
