@@ -134,8 +134,13 @@ __global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T
         for (int e = 0; e < 8; ++e) {
             ss = fmaf(h[e], h[e], ss);
             h[e] *= w[e];
-            const uint32_t m = bits_of_f32(h[e]) & 0x7FFFFFFFu;
-            top = m > top ? m : top;
+        }
+        if (scaled) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t m = bits_of_f32(h[e]) & 0x7FFFFFFFu;
+                top = m > top ? m : top;
+            }
         }
         norm_reduce(T, part, partu, slot, ss, top, scaled);
         if (r >= a.rows) continue;

@@ -38,39 +38,53 @@ PNN_HD uint32_t bits_of_f32(float v) { return __builtin_bit_cast(uint32_t, v); }
 //    counts the run and puts exponent and fraction at the top of the significand, adding 2^23 to a binary32 puts a significand behind
 //    a run of zeros and rounds it, nearest with ties to even.
 
+//
+// The parts of both directions that leave zero and NaR (NaN) aside:
+
+// Value; 0 and NaR give garbage and y == 0.  A negative pattern needs no negation: without its sign it is the negated magnitude, so T changes sign.
+PNN_HD float posit_value_regular(uint32_t p, ElemFmt f, uint32_t& y) {
+    const uint32_t u = p << (32 - f.n), x = u << 1;             // sign on top; regime on top; zeros below the pattern
+    y = (uint32_t)((int32_t)x < 0 ? 0 - x : x);
+    const uint32_t t = (bits_of_f32((float)y) << f.es) - (158u << (23 + f.es));
+    const uint32_t s = (uint32_t)((int32_t)(x ^ u) >> 31);
+    const uint32_t mag = (t ^ s) + ((127u << 23) - s);
+    return f32_of_bits((mag & 0x7FFFFFFFu) | (u & 0x80000000u));
+}
+
+// Nearest pattern, in the low n bits, for a finite nonzero value; `value` receives what it stands for.
+template <bool VALUE>
+PNN_HD uint32_t posit_nearest_regular(float v, ElemFmt f, float& value) {
+    const uint32_t bits = bits_of_f32(v), t = (bits & 0x7FFFFFFFu) - (127u << 23), st = (uint32_t)((int32_t)t >> 31);
+    const int32_t range = (int32_t)((uint32_t)((f.n - 2) << f.es) << 23);
+    int32_t below = (int32_t)t < 0 ? (int32_t)t : -(int32_t)t;
+    below = below > -range ? below : -range;
+    // es bits leave the significand; they stay as "not zero" in its last ones, far below any cut
+    const uint32_t g = (uint32_t)(below >> f.es) | ((uint32_t)below & ((1u << f.es) - 1u));
+    // the rounded integer negated for a value of 1 and above, and for a negative one: as two's complement below 1.5 2^23
+    const uint32_t exponent = (uint32_t)(127 + f.n - 2) << 23;
+    const float cut = f32_of_bits(((g + exponent) & 0x7FFFFFFFu) | ((bits ^ ~t) & 0x80000000u)) + 12582912.f;
+    if (VALUE) {
+        const uint32_t r = ((bits_of_f32(cut - 12582912.f) & 0x7FFFFFFFu) - exponent) << f.es;
+        const uint32_t mag = (r ^ ~st) + ((127u << 23) - ~st);
+        value = f32_of_bits((mag & 0x7FFFFFFFu) | (bits & 0x80000000u));
+    }
+    return bits_of_f32(cut) ^ (~st & (1u << (f.n - 1)));
+}
+
 // Value of a posit of at most 16 bits, exact (at most 13 significant bits, |scale| <= 40); NaR gives NaN.
 PNN_HD float posit_value(uint32_t p, ElemFmt f) {
-    const int32_t u = (int32_t)(p << (32 - f.n));               // sign on top; zeros below the pattern
-    const uint32_t x = (uint32_t)(u < 0 ? 0 - (uint32_t)u : (uint32_t)u) << 1;  // regime on top
-    const uint32_t s = (uint32_t)((int32_t)x >> 31);            // 1 and above
-    const uint32_t y = (x ^ s) - s;
-    const uint32_t t = (bits_of_f32((float)y) << f.es) - (158u << (23 + f.es));
-    const uint32_t mag = (t ^ s) + ((127u << 23) - s);
-    const uint32_t v = (mag & 0x7FFFFFFFu) | ((uint32_t)u & 0x80000000u);
-    return f32_of_bits(y == 0u ? (uint32_t)(u >> 9) : v);        // zero, or a quiet NaN
+    uint32_t y;
+    const float v = posit_value_regular(p, f, y);
+    return y == 0u ? f32_of_bits((p >> (f.n - 1)) & 1u ? 0x7FC00000u : 0u) : v;
 }
 
 // Nearest posit of at most 16 bits, ties to the even pattern, never zero or NaR for a finite nonzero value; NaN and infinities
 // give NaR.  `value` receives what the pattern stands for.
 template <bool VALUE>
 PNN_HD uint32_t posit_nearest(float v, ElemFmt f, float& value) {
-    const uint32_t bits = bits_of_f32(v), ah = bits & 0x7FFFFFFFu;
-    const int32_t range = (int32_t)((uint32_t)((f.n - 2) << f.es) << 23), raw = (int32_t)(ah - (127u << 23));
-    const int32_t t = raw < -range ? -range : (raw > range ? range : raw);
-    const int32_t below = t < 0 ? t : -t;
-    // es bits leave the significand; they stay as "not zero" in its last ones, far below any cut
-    const uint32_t g = (uint32_t)(below >> f.es) | ((uint32_t)below & ((1u << f.es) - 1u));
-    const float cut = f32_of_bits(g + ((uint32_t)(127 + f.n - 2) << 23)) + 8388608.f;
-    const uint32_t st = (uint32_t)(t >> 31), sb = (uint32_t)((int32_t)bits >> 31);
-    const uint32_t m = ~(st ^ sb);                                // negate: for a value of 1 and above, and for a negative one
-    const uint32_t p = ((bits_of_f32(cut) ^ m) - m + (~st & (1u << (f.n - 1)))) & ((1u << f.n) - 1u);
+    const uint32_t p = posit_nearest_regular<VALUE>(v, f, value) & ((1u << f.n) - 1u), ah = bits_of_f32(v) & 0x7FFFFFFFu;
     const bool zero = ah == 0u, nar = ah >= 0x7F800000u;
-    if (VALUE) {
-        const uint32_t r = (bits_of_f32(cut - 8388608.f) - ((uint32_t)(127 + f.n - 2) << 23)) << f.es;
-        const uint32_t mag = (r ^ ~st) - ~st + (127u << 23);
-        const uint32_t w = (mag & 0x7FFFFFFFu) | (bits & 0x80000000u);
-        value = f32_of_bits(zero ? 0u : (nar ? 0x7FC00000u : w));
-    }
+    if (VALUE) value = zero ? 0.f : (nar ? f32_of_bits(0x7FC00000u) : value);
     return zero ? 0u : (nar ? 1u << (f.n - 1) : p);
 }
 PNN_HD uint32_t posit_nearest(float v, ElemFmt f) {
@@ -156,13 +170,27 @@ __device__ __forceinline__ void load8(Raw8& r, const void* p, int64_t i, int kin
     }
 }
 
+__device__ __forceinline__ uint32_t pattern8(const Raw8& r, int e, int kind) {
+    return kind == KIND_POSIT_U8 ? (r.w[e / 4] >> (8 * (e & 3))) & 0xFFu : (e & 1 ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xFFFFu);
+}
+
 __device__ __forceinline__ void values8(float (&v)[8], const Raw8& r, int kind, ElemFmt f) {
-    if (kind == KIND_POSIT_U8) {
+    if (kind == KIND_POSIT_U8 || kind == KIND_POSIT_U16) {
+        // zeros and NaR are looked for once for all eight
+        uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = posit_value((r.w[e / 4] >> (8 * (e & 3))) & 0xFFu, f);
-    } else if (kind == KIND_POSIT_U16) {
+        for (int e = 0; e < 8; ++e) {
+            uint32_t y;
+            v[e] = posit_value_regular(pattern8(r, e, kind), f, y);
+            least = y < least ? y : least;
+        }
+        if (least == 0u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = posit_value(e & 1 ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xFFFFu, f);
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t p = pattern8(r, e, kind);
+                v[e] = p == 0u ? 0.f : (p == 1u << (f.n - 1) ? f32_of_bits(0x7FC00000u) : v[e]);
+            }
+        }
     } else if (kind == KIND_BF16) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = f32_of_bits(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
@@ -188,19 +216,35 @@ __device__ __forceinline__ void raw8(Raw8& r, float (&v)[8], int kind, ElemFmt f
             }
         }
     } else {
-        uint32_t q[8];
+        uint32_t q[8], worst = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float back = 0.f;
-            q[e] = posit_nearest<VALUE>(v[e], f, back);
-            if (VALUE) v[e] = back;
+            const uint32_t odd = (bits_of_f32(v[e]) & 0x7FFFFFFFu) - 1u;  // zero, infinities and NaN: 0x7F7FFFFF and above
+            worst = odd > worst ? odd : worst;
         }
-        if (kind == KIND_POSIT_U8) {
-            r.w[0] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-            r.w[1] = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+        if (worst < 0x7F7FFFFFu) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float back = 0.f;
+                q[e] = posit_nearest_regular<VALUE>(v[e], f, back);
+                if (VALUE) v[e] = back;
+            }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r.w[e] = q[2 * e] | q[2 * e + 1] << 16;
+            for (int e = 0; e < 8; ++e) {
+                float back = 0.f;
+                q[e] = posit_nearest<VALUE>(v[e], f, back);
+                if (VALUE) v[e] = back;
+            }
+        }
+        if (kind == KIND_POSIT_U8) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                r.w[e] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * e + 3], q[4 * e + 2], 0x0C0C0400u), __builtin_amdgcn_perm(q[4 * e + 1], q[4 * e], 0x0C0C0400u), 0x05040100u);
+        } else {
+            const uint32_t mask = ((1u << f.n) - 1u) * 0x10001u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.w[e] = __builtin_amdgcn_perm(q[2 * e + 1], q[2 * e], 0x05040100u) & mask;
         }
     }
 }
