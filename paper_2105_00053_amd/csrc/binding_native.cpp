@@ -384,10 +384,19 @@ PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_NONE;
 }
 
+}  // namespace
+
+#include "binding_lm.h"
+
+namespace {
+
 #define PNN_METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PNN_METHOD("init", init), PNN_METHOD("gemm", gemm), PNN_METHOD("conv", conv), PNN_METHOD("round", round_to),
                          PNN_METHOD("convert", convert), PNN_METHOD("relu", relu), PNN_METHOD("relu_bwd", relu_bwd), PNN_METHOD("maxpool_fwd", maxpool_fwd),
-                         PNN_METHOD("maxpool_bwd", maxpool_bwd), PNN_METHOD("avgpool", avgpool), {nullptr, nullptr, 0, nullptr}};
+                         PNN_METHOD("maxpool_bwd", maxpool_bwd), PNN_METHOD("avgpool", avgpool),
+                         PNN_METHOD("init_lm", init_lm), PNN_METHOD("rmsnorm_fwd", rmsnorm_fwd), PNN_METHOD("rmsnorm_bwd", rmsnorm_bwd), PNN_METHOD("scale_rows", scale_rows),
+                         PNN_METHOD("attention_fwd", attention_fwd), PNN_METHOD("attention_bwd", attention_bwd), PNN_METHOD("logprob_fwd", logprob_fwd),
+                         PNN_METHOD("logprob_bwd", logprob_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "positnn_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -9,6 +9,7 @@ import math
 
 import torch
 
+from . import binding
 from .binding import ELEM_SIZE, FORMAT_CODES, PositError, TORCH_DTYPE, _SAME_SIZE, _check, _stream, load
 
 BF16 = 102
@@ -47,8 +48,29 @@ def _load():
             getattr(L, name).restype = ci
         for name in ("posit_rmsnorm_bwd_workspace", "posit_attention_workspace", "posit_token_logprob_workspace"):
             getattr(L, name).restype = sz
+        if binding._native is not None:
+            binding._native.init_lm(*(ctypes.cast(getattr(L, name), vp).value for name in _NATIVE_ORDER))
         _lib = L
     return _lib
+
+
+# As in binding.py, a call goes to the extension module first, which returns None for whatever it does not take.
+_NATIVE_ORDER = ("posit_rmsnorm_fwd", "posit_rmsnorm_bwd", "posit_rmsnorm_bwd_workspace", "posit_scale_rows", "posit_attention_fwd", "posit_attention_bwd",
+                 "posit_attention_workspace", "posit_token_logprob_fwd", "posit_token_logprob_workspace", "posit_token_logprob_bwd")
+
+
+def _ready():
+    """(the extension module, the current stream), or (None, None) where the Python code takes the call."""
+    if _lib is None:
+        _load()
+    stream = binding._ready()
+    return (None, None) if stream is None else (binding._native, stream)
+
+
+def _returned(r):
+    if r.__class__ is int:
+        _check(r)
+    return r
 
 
 def _code(f):
@@ -110,6 +132,11 @@ def posit_rmsnorm_fwd(x, w, fx, fw, fy, eps=1e-6, res=None, fres=None, scaled=Fa
     """(y, scale, res_out, rstd) of the RMS norm of x (+ res): scale is None unless `scaled`, res_out None without res."""
     fx, fw, fy = _code(fx), _code(fw), _code(fy)
     fres = fx if fres is None else _code(fres)
+    native, st = _ready()
+    if native is not None:
+        r = native.rmsnorm_fwd(st, fx, fw, fy, fres, 1 if scaled else 0, float(eps), x, w, res)
+        if r is not None:
+            return _returned(r)
     xp, ldx = _matrix(x, fx, "x")
     rows, cols = x.shape
     res_out, rp, ldr, op, ldo = None, None, 0, None, 0
@@ -128,6 +155,11 @@ def posit_rmsnorm_bwd(dy, h, w, rstd, fd, fh, fw, fdx, fdw, dres=None, fdres=Non
     """(dx, dw) for the gradient dy of the unscaled output; h is the normalised stream (res_out, or x), dres the gradient past the norm."""
     fd, fh, fw, fdx, fdw = _code(fd), _code(fh), _code(fw), _code(fdx), _code(fdw)
     fdres = fd if fdres is None else _code(fdres)
+    native, st = _ready()
+    if native is not None and workspace is None:
+        r = native.rmsnorm_bwd(st, fd, fh, fw, fdx, fdw, fdres, 1 if want_dw else 0, dy, h, w, rstd, dres)
+        if r is not None:
+            return _returned(r)
     dp, lddy = _matrix(dy, fd, "dy")
     rows, cols = dy.shape
     hp, ldh = _matrix(h, fh, "h", dy.shape)
@@ -146,11 +178,20 @@ def posit_rmsnorm_bwd(dy, h, w, rstd, fd, fh, fw, fdx, fdw, dres=None, fdres=Non
 def posit_scale_rows(x, scale, fin, fout):
     """scale[r] * x[r], rounded to fout."""
     fin, fout = _code(fin), _code(fout)
+    native, st = _ready()
+    if native is not None:
+        r = native.scale_rows(st, fin, fout, x, scale)
+        if r is not None:
+            return _returned(r)
     xp, ldx = _matrix(x, fin, "x")
     rows, cols = x.shape
     y = torch.empty((rows, cols), dtype=_dtype(fout), device=x.device)
     _check(_load().posit_scale_rows(_stream(), fin, fout, rows, cols, xp, ldx, _vector(scale, torch.float32, rows, "scale"), y.data_ptr(), cols))
     return y
+
+
+def _scale(scale, q):
+    return 1.0 / math.sqrt(max(q.shape[3], 1)) if scale is None else float(scale)
 
 
 def _attention(q, k, v, fq, fkv, scale, window, sinks, lens):
@@ -162,7 +203,7 @@ def _attention(q, k, v, fq, fkv, scale, window, sinks, lens):
     lk, hkv = k.shape[1:3]
     if tuple(k.shape) != (b, lk, hkv, d) or tuple(v.shape) != (b, lk, hkv, d):
         raise PositError("q, k and v have shapes %s, %s, %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
-    desc = AttentionDesc(b, hq, hkv, lq, lk, d, window, sinks, 1.0 / math.sqrt(max(d, 1)) if scale is None else scale,
+    desc = AttentionDesc(b, hq, hkv, lq, lk, d, window, sinks, _scale(scale, q),
                          *q.stride()[:3], *k.stride()[:3], *v.stride()[:3])
     return desc, _vector(lens, torch.int32, b, "lens")
 
@@ -174,6 +215,11 @@ def posit_attention_workspace(which, fkv, desc):
 def posit_attention_fwd(q, k, v, fq, fkv, fout, scale=None, window=0, sinks=0, lens=None, fcopy=None, workspace=None):
     """(o, lse, o_copy) for q [b][i][h][d], k and v [b][j][h'][d]; o_copy is o rounded to fcopy, None without it.  scale: 1 / sqrt(d) by default."""
     fq, fkv, fout = _code(fq), _code(fkv), _code(fout)
+    native, st = _ready()
+    if native is not None and workspace is None and isinstance(q, torch.Tensor) and q.dim() == 4:
+        r = native.attention_fwd(st, fq, fkv, fout, window, sinks, -1 if fcopy is None else _code(fcopy), _scale(scale, q), q, k, v, lens)
+        if r is not None:
+            return _returned(r)
     desc, lp = _attention(q, k, v, fq, fkv, scale, window, sinks, lens)
     b, lq, hq, d = q.shape
     o = torch.empty((b, lq, hq, d), dtype=_dtype(fout), device=q.device)
@@ -189,6 +235,11 @@ def posit_attention_fwd(q, k, v, fq, fkv, fout, scale=None, window=0, sinks=0, l
 def posit_attention_bwd(do, q, k, v, o, lse, fd, fq, fkv, fo, fout, scale=None, window=0, sinks=0, lens=None, workspace=None):
     """(dq, dk, dv) for the gradient do of the output; o (dense, in fo) and lse come from the forward call."""
     fd, fq, fkv, fo, fout = _code(fd), _code(fq), _code(fkv), _code(fo), _code(fout)
+    native, st = _ready()
+    if native is not None and workspace is None and isinstance(q, torch.Tensor) and q.dim() == 4:
+        r = native.attention_bwd(st, fd, fq, fkv, fo, fout, window, sinks, _scale(scale, q), do, q, k, v, o, lse, lens)
+        if r is not None:
+            return _returned(r)
     desc, lp = _attention(q, k, v, fq, fkv, scale, window, sinks, lens)
     b, lq, hq, d = q.shape
     lk, hkv = k.shape[1:3]
@@ -215,6 +266,11 @@ def posit_attention_bwd(do, q, k, v, o, lse, fd, fq, fkv, fo, fout, scale=None, 
 def posit_token_logprob_fwd(logits, targets, fz, inv_temperature=1.0, top=0, workspace=None):
     """(logprob, lse, entropy, top_logprob, top_index) of each row; logprob is None without targets, the last two without `top`."""
     fz = _code(fz)
+    native, st = _ready()
+    if native is not None and workspace is None:
+        r = native.logprob_fwd(st, fz, top, float(inv_temperature), logits, targets)
+        if r is not None:
+            return _returned(r)
     zp, ldz = _matrix(logits, fz, "logits")
     rows, vocab = logits.shape
     if vocab == 0 and rows > 0:
@@ -234,6 +290,11 @@ def posit_token_logprob_fwd(logits, targets, fz, inv_temperature=1.0, top=0, wor
 def posit_token_logprob_bwd(logits, targets, lse, entropy, g_logprob, g_entropy, fz, fg, inv_temperature=1.0):
     """Gradient with respect to the logits, for those of logprob and entropy (each may be None)."""
     fz, fg = _code(fz), _code(fg)
+    native, st = _ready()
+    if native is not None:
+        r = native.logprob_bwd(st, fz, fg, float(inv_temperature), logits, targets, lse, entropy, g_logprob, g_entropy)
+        if r is not None:
+            return _returned(r)
     zp, ldz = _matrix(logits, fz, "logits")
     rows, vocab = logits.shape
     f32 = torch.float32
