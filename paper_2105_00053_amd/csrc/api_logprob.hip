@@ -2,8 +2,8 @@
 //
 // Forward.  A workgroup takes a row, or a part of one where rows are few or long, into registers (64 words a thread) and goes
 // over it there: maximum, then the sums of e^(z-m) and of e^(z-m) (z-m), then the alternatives; memory is read once.  A second kernel joins parts.
-//  - 8-bit posits: 256 values at most, so a row is its histogram (in LDS, one copy of each bin for every bank: additions without
-//    conflicts) and the sums are over 256 bins: no decoding, no exponential per logit.
+//  - 8-bit posits: 256 values at most, so a row is its histogram (in LDS, 16 copies of each bin, so that the lanes of a wave meet
+//    few conflicts) and the sums are over 256 bins: no decoding, no exponential per logit; the k-th largest value is there too.
 //  - 16-bit posits: the order of posits is that of their patterns as integers, so maximum and NaR come from packed integer instructions.
 // Alternatives.  Each thread's largest logit (with the place of its vector) is sorted among the 256: the k-th largest of these
 // bounds the k-th largest of all from below, and few logits are above it (about k + k^2 / 512 for random ones).  Those are collected and ranked by
@@ -43,7 +43,7 @@ __device__ __forceinline__ float lp_value(uint32_t order, int kind, ElemFmt f) {
     return f32_of_bits(order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
 
-constexpr int LP_LIST = 1024;
+constexpr int LP_LIST = 1024, LP_COPIES = 16;
 struct LogprobTop {
     lp_key sorted[4][64];
     lp_key list[LP_LIST];
@@ -52,31 +52,43 @@ struct LogprobTop {
     int count;
 };
 
-__device__ __forceinline__ lp_key lp_swap(lp_key v, int mask) {
-    const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, mask, 64), hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), mask, 64);
-    return (lp_key)hi << 32 | lo;
+// The key of lane ^ MASK.  Through the vector unit where its lane shifts reach (a shuffle through LDS takes many times as long).
+template <int MASK>
+__device__ __forceinline__ uint32_t lp_swap32(uint32_t v) {
+    if constexpr (MASK == 1) return lane_shift<0xB1, 0xF>(v, 0u);
+    else if constexpr (MASK == 2) return lane_shift<0x4E, 0xF>(v, 0u);
+    else if constexpr (MASK == 3) return lane_shift<0x1B, 0xF>(v, 0u);
+    else if constexpr (MASK == 4) return lp_swap32<3>(lp_swap32<7>(v));
+    else if constexpr (MASK == 7) return lane_shift<0x141, 0xF>(v, 0u);
+    else if constexpr (MASK == 8) return lane_shift<0x128, 0xF>(v, 0u);
+    else if constexpr (MASK == 15) return lane_shift<0x140, 0xF>(v, 0u);
+    else return (uint32_t)__shfl_xor((int)v, MASK, 64);
+}
+template <int MASK>
+__device__ __forceinline__ lp_key lp_swap(lp_key v) { return (lp_key)lp_swap32<MASK>((uint32_t)(v >> 32)) << 32 | lp_swap32<MASK>((uint32_t)v); }
+
+// One step of sorting a wave's keys, the largest to the lowest lane: of lane and lane ^ MASK, the one without TOP (MASK's highest bit) keeps the larger.
+template <int MASK, int TOP>
+__device__ __forceinline__ lp_key lp_step(lp_key v) {
+    const lp_key o = lp_swap<MASK>(v);
+    const bool first = (threadIdx.x & TOP) == 0;
+    return first == (v > o) ? v : o;
+}
+__device__ __forceinline__ lp_key lp_sort(lp_key v) {
+    v = lp_step<1, 1>(v);
+    v = lp_step<1, 1>(lp_step<3, 2>(v));
+    v = lp_step<1, 1>(lp_step<2, 2>(lp_step<7, 4>(v)));
+    v = lp_step<1, 1>(lp_step<2, 2>(lp_step<4, 4>(lp_step<15, 8>(v))));
+    v = lp_step<1, 1>(lp_step<2, 2>(lp_step<4, 4>(lp_step<8, 8>(lp_step<31, 16>(v)))));
+    return lp_step<1, 1>(lp_step<2, 2>(lp_step<4, 4>(lp_step<8, 8>(lp_step<16, 16>(lp_step<63, 32>(v))))));
 }
 
-// The k largest keys of a workgroup, in order, in sh.result (0 where there are no more).  `best`: each thread's largest, or a key that one
-// of its own, at most `slack` below it, has; visit(bound, f) calls f with the thread's keys from `bound` up.
-template <class Visit>
-__device__ __forceinline__ void lp_select(LogprobTop& sh, lp_key best, uint32_t slack, int k, Visit visit) {
+// A bound from below for the k-th largest key of a workgroup, in sh.bound behind the next barrier (0: none).  `best`: each thread's largest, or a key that
+// one of its own, at most `slack` below it, has.
+__device__ __forceinline__ void lp_bound(LogprobTop& sh, lp_key best, uint32_t slack, int k) {
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-#pragma unroll
-    for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-        for (int step = size / 2; step >= 1; step /= 2) {
-            const lp_key other = lp_swap(best, step);
-            const bool up = (lane & size) != 0 && size < 64, first = (lane & step) == 0;
-            best = (first != up) == (best > other) ? best : other;
-        }
-    __syncthreads();
+    best = lp_sort(best);
     sh.sorted[w][lane] = best;
-    if (t < 64) sh.result[t] = 0;
-    if (t == 0) {
-        sh.bound = 0;
-        sh.count = 0;
-    }
     __syncthreads();
     int rank = lane;
     for (int o = 1; o < 4; ++o) {
@@ -88,6 +100,13 @@ __device__ __forceinline__ void lp_select(LogprobTop& sh, lp_key best, uint32_t 
         rank += at;
     }
     if (rank == k - 1 && best != 0) sh.bound = best - slack;
+}
+
+// The k largest keys of a workgroup, in order, in sh.result (0 where there are no more), given sh.bound; visit(bound, f) calls f with the thread's keys from
+// `bound` up.
+template <class Visit>
+__device__ __forceinline__ void lp_select(LogprobTop& sh, int k, Visit visit) {
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     __syncthreads();
     const lp_key bound = sh.bound;
     visit(bound, [&](lp_key key) {
@@ -110,7 +129,7 @@ __device__ __forceinline__ void lp_select(LogprobTop& sh, lp_key best, uint32_t 
             visit(0, [&](lp_key key) { b = key < last && key > b ? key : b; });
 #pragma unroll
             for (int m = 32; m >= 1; m >>= 1) {
-                const lp_key o = lp_swap(b, m);
+                const lp_key o = (lp_key)(uint32_t)__shfl_xor((int)(uint32_t)(b >> 32), m, 64) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)b, m, 64);
                 b = o > b ? o : b;
             }
             __syncthreads();
@@ -123,6 +142,14 @@ __device__ __forceinline__ void lp_select(LogprobTop& sh, lp_key best, uint32_t 
         }
     }
     __syncthreads();
+}
+// before lp_bound, with a barrier between
+__device__ __forceinline__ void lp_clear(LogprobTop& sh) {
+    if (threadIdx.x < 64) sh.result[threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        sh.bound = 0;
+        sh.count = 0;
+    }
 }
 
 __device__ __forceinline__ float lp_block_sum(float v, float* part) {
@@ -171,7 +198,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     constexpr bool POSIT = K == KIND_POSIT_U8 || K == KIND_POSIT_U16;
     __shared__ float part[4];
     __shared__ LogprobTop sh;
-    __shared__ uint32_t hist[K == KIND_POSIT_U8 ? 8192 : 1];
+    __shared__ uint32_t hist[K == KIND_POSIT_U8 ? 256 * LP_COPIES : 1];
     const int t = threadIdx.x;
     const int64_t row = blockIdx.x / (unsigned)a.parts;
     const int p = blockIdx.x - (unsigned)row * a.parts;
@@ -179,6 +206,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     const int n = (int)(a.vocab - begin < a.span ? a.vocab - begin : a.span), vectors = n / 8, rest = n - vectors * 8;
     const char* const src = (const char*)a.z + (row * a.ldz + begin) * B;
     const float inf = f32_of_bits(0x7F800000u);
+    lp_clear(sh);
     uint32_t raw[NC][W];
 #pragma unroll
     for (int c = 0; c < NC; ++c)
@@ -189,15 +217,20 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     if (extra) one = B == 1 ? ((const uint8_t*)src)[vectors * 8 + t] : B == 2 ? ((const uint16_t*)src)[vectors * 8 + t] : ((const uint32_t*)src)[vectors * 8 + t];
     if (K == KIND_POSIT_U8) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) ((uint4*)hist)[c * 256 + t] = make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < LP_COPIES / 4; ++c) ((uint4*)hist)[c * 256 + t] = make_uint4(0, 0, 0, 0);
         __syncthreads();
     }
 
     auto element = [&](const uint32_t* w, int e) -> uint32_t { return B == 4 ? w[e] : (w[e * B / 4] >> (8 * B * (e % (4 / B)))) & (B == 1 ? 0xFFu : 0xFFFFu); };
-    auto value = [&](uint32_t x) -> float { return value_of<K>(x, a.f); };
+    // 16-bit posits: zero as 2^-60 or less (es is 1 or 2), which no sum here sees; NaR is looked for by itself
+    auto value = [&](uint32_t x) -> float {
+        uint32_t y;
+        return K == KIND_POSIT_U16 ? posit_value_regular(x, a.f, y) : value_of<K>(x, a.f);
+    };
     auto order = [&](uint32_t x) -> uint32_t { return POSIT ? lp_order_posit(x, a.f) : lp_order(value(x)); };
-    // the largest of a vector, as its order
-    auto vector_top = [&](const uint32_t* w) -> uint32_t {
+    // the largest of a vector, as its order; for 16-bit posits the smallest too (NaR is the smallest of all)
+    lp_pair least = {0, 0};
+    auto vector_top = [&](const uint32_t* w, bool low) -> uint32_t {
         if constexpr (POSIT) {
             const int shift = 16 - a.f.n;  // patterns of 10 and 12 bits to the top of their half words
             lp_pair m;
@@ -210,6 +243,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
                     x = __builtin_elementwise_max(x, y);
                 } else {
                     x = __builtin_bit_cast(lp_pair, w[i]) << (short)shift;
+                    if (low) least = __builtin_elementwise_min(least, x);
                 }
                 m = i ? __builtin_elementwise_max(m, x) : x;
             }
@@ -223,49 +257,44 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
         }
     };
 
-    // maximum, and each thread's largest with the place of its vector
-    uint32_t top = 0, low = 0xFFFFFFFFu, best = 0;
+    // each thread's largest, with the place of its vector
+    uint32_t best = 0;
     int at = 0;
+    auto look = [&](bool low) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-        if (c * 256 + t >= vectors) continue;
-        if (K == KIND_POSIT_U8) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) atomicAdd(&hist[element(raw[c], e) * 32 + (t & 31)], 1u);
-            if (a.top == 0) continue;
-        }
-        const uint32_t v = vector_top(raw[c]);
-        if (v > best) {
-            best = v;
-            at = (c * 256 + t) * 8;
-        }
-        if (K == KIND_POSIT_U16) {
-#pragma unroll
-            for (int i = 0; i < W; ++i) {
-                const lp_pair x = __builtin_bit_cast(lp_pair, raw[c][i]) << (short)(16 - a.f.n);
-                low = (x.x == -32768 || x.y == -32768) ? 0u : low;
+        for (int c = 0; c < NC; ++c) {
+            if (c * 256 + t >= vectors) continue;
+            const uint32_t v = vector_top(raw[c], low);
+            if (v > best) {
+                best = v;
+                at = (c * 256 + t) * 8;
             }
         }
-    }
-    if (extra) {
-        if (K == KIND_POSIT_U8) atomicAdd(&hist[one * 32 + (t & 31)], 1u);
-        const uint32_t v = order(one);
-        if (K == KIND_POSIT_U16 && one == 1u << (a.f.n - 1)) low = 0;
-        if (v > best) {
-            best = v;
-            at = vectors * 8 + t;
+        if (extra) {
+            const uint32_t v = order(one);
+            if (v > best) {
+                best = v;
+                at = vectors * 8 + t;
+            }
         }
-    }
-    top = best;
+    };
+    bool bounded = false;  // the histogram knows the k-th largest
     float m, s = 0.f, u = 0.f;
     bool bad = false;
     if (K == KIND_POSIT_U8) {
-        // thread t is bin t
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            if (c * 256 + t >= vectors) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) atomicAdd(&hist[element(raw[c], e) * LP_COPIES + (t & (LP_COPIES - 1))], 1u);
+        }
+        if (extra) atomicAdd(&hist[one * LP_COPIES + (t & (LP_COPIES - 1))], 1u);
         __syncthreads();
+        // thread t is bin t
         uint32_t count = 0;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const uint4 x = ((const uint4*)hist)[t * 8 + ((c + t) & 7)];
+        for (int c = 0; c < LP_COPIES / 4; ++c) {
+            const uint4 x = ((const uint4*)hist)[t * (LP_COPIES / 4) + ((c + t) & (LP_COPIES / 4 - 1))];
             count += x.x + x.y + x.z + x.w;
         }
         const bool nar = t == 128;
@@ -275,9 +304,28 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
         const float d = v - m, e = count > 0 ? (float)count * __builtin_amdgcn_exp2f(d * LP_LOG2E) : 0.f;
         s = lp_block_sum(e, part);
         u = lp_block_sum(e > 0.f ? e * d : 0.f, part);
+        if (a.top > 0) {
+            // logits in the bins from the largest value down to thread t's, 127 - t for what is not negative: where they reach k is the bound
+            uint32_t* const down = hist;
+            down[(127 - t) & 255] = count;
+            __syncthreads();
+            const uint32_t mine = down[t];
+            uint32_t sum = mine;
+#define PNN_STEP(CTRL, ROWS) sum += lane_shift<CTRL, ROWS>(sum, 0u);
+            PNN_STEP(0x111, 0xF) PNN_STEP(0x112, 0xF) PNN_STEP(0x114, 0xF) PNN_STEP(0x118, 0xF) PNN_STEP(0x142, 0xA) PNN_STEP(0x143, 0xC)
+#undef PNN_STEP
+            if ((t & 63) == 63) down[256 + (t >> 6)] = sum;
+            __syncthreads();
+            for (int w = 0; w < (t >> 6); ++w) sum += down[256 + w];
+            const bool here = sum >= (uint32_t)a.top && sum - mine < (uint32_t)a.top;
+            if (here) sh.bound = (lp_key)lp_order_posit((uint32_t)(127 - t) & 0xFFu, a.f) << 32;
+            bounded = !__syncthreads_or(here && sum > (uint32_t)LP_LIST);  // too many of that value for the list
+            if (!bounded && t == 0) sh.bound = 0;
+        }
     } else {
-        const uint32_t t0 = wave_max_u32(top);
-        if (POSIT) bad = __syncthreads_or(low == 0u);
+        look(K == KIND_POSIT_U16);
+        const uint32_t t0 = wave_max_u32(best);
+        if (POSIT) bad = __syncthreads_or(least.x == -32768 || least.y == -32768 || (extra && one == 1u << (a.f.n - 1)));
         m = lp_block_max(t0 == 0 ? -inf : lp_value(t0, K, a.f) * a.tau, part);
         if (m > -inf) {
 #pragma unroll
@@ -320,7 +368,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 if (c * 256 + t >= vectors) continue;
-                if (vector_top(raw[c]) < (uint32_t)(bound >> 32)) continue;
+                if (vector_top(raw[c], false) < (uint32_t)(bound >> 32)) continue;
                 if constexpr (B == 4) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -343,8 +391,13 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
                 if (key != 0 && key >= bound) f(key);
             }
         };
-        const bool any = POSIT ? best != 0 : best > LP_ORDER_OF_MINUS_INF;
-        lp_select(sh, any ? (lp_key)best << 32 | (uint32_t)~(uint32_t)(begin + at) : 0, 7, a.top, visit);
+        if (!bounded) {
+            if (K == KIND_POSIT_U8) look(false);
+            const bool any = POSIT ? best != 0 : best > LP_ORDER_OF_MINUS_INF;
+            __syncthreads();
+            lp_bound(sh, any ? (lp_key)best << 32 | (uint32_t)~(uint32_t)(begin + at) : 0, 7, a.top);
+        }
+        lp_select(sh, a.top, visit);
     }
     if (a.parts == 1) {
         lp_outputs(a, row, m, s, u, bad, sh.result);
@@ -365,6 +418,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobFwd a) {
     const float4* const st = a.part_stats + row * a.parts;
     float m = -inf;
     bool bad = false;
+    lp_clear(sh);
     for (int i = t; i < a.parts; i += 256) {
         m = fmaxf(m, st[i].x);
         bad |= st[i].w != 0.f;
@@ -386,7 +440,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobFwd a) {
         const int64_t n = (int64_t)a.parts * a.top;
         lp_key best = 0;
         for (int64_t i = t; i < n; i += 256) best = keys[i] > best ? keys[i] : best;
-        lp_select(sh, best, 0, a.top, [&](lp_key bound, auto f) {
+        lp_bound(sh, best, 0, a.top);
+        lp_select(sh, a.top, [&](lp_key bound, auto f) {
             for (int64_t i = t; i < n; i += 256)
                 if (keys[i] != 0 && keys[i] >= bound) f(keys[i]);
         });
