@@ -109,7 +109,7 @@ void launch_fwd(hipStream_t st, const Plan& p, const AttnFwd& a) {
 template <int DB, bool TWO>
 void launch_bwd_of(hipStream_t st, const Plan& p, const AttnBwd& a) {
     if (p.s.LQ > 0) hipLaunchKernelGGL((attn_dq_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.qblocks / 4))), dim3(256), 0, st, a);
-    if (p.s.LK > 0) hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 4))), dim3(256), 0, st, a);
+    if (p.s.LK > 0) hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 2))), dim3(256), 0, st, a);
 }
 
 template <bool TWO>
@@ -143,7 +143,7 @@ extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attent
     const Plan p = make_plan(*desc);
     const TokenPlan t = token_plan(*desc);
     if (which == 0 && t.use) return (size_t)t.bytes;
-    if (which == 0) return (size_t)(p.q_bytes + 2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
+    if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
     return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4));
 }
 
@@ -182,18 +182,16 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
         if (tp.parts > 1) hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)p.s.rows, (unsigned)d.HKV, (unsigned)d.B), dim3(128), 0, st, a);
         return hip_status(hipGetLastError());
     }
-    uint4* const wq = (uint4*)workspace;
-    uint4* const wk = wq + p.q_bytes / 16;
+    uint4* const wk = (uint4*)workspace;
     uint4* const wv = wk + p.k_bytes / 16;
     int32_t* const flags = (int32_t*)(wv + p.k_bytes / 16);
     AttnPack pack = {};
     pack.B = (int)d.B; pack.HKV = (int)d.HKV; pack.D = (int)d.D;
-    pack.item[0] = {q, d.qb, d.ql, d.qh, p.s.rows, p.s.qblocks, wq, nullptr, p.s.G, kind_of(fq), elem_fmt(fq), nullptr};
-    pack.item[1] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr};
-    pack.item[2] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, nullptr, wv, 1, kind_of(fkv), elem_fmt(fkv), flags};
-    launch_pack(st, p, pack, 3);
+    pack.item[0] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr};
+    pack.item[1] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, nullptr, wv, 1, kind_of(fkv), elem_fmt(fkv), flags};
+    launch_pack(st, p, pack, 2);
     AttnFwd a = {};
-    a.s = p.s; a.q = wq; a.k = wk; a.v = wv; a.o = o; a.copy = o_copy; a.lse = lse;
+    a.s = p.s; a.q = q; a.qb = d.qb; a.ql = d.ql; a.qh = d.qh; a.kq = kind_of(fq); a.fq = elem_fmt(fq); a.k = wk; a.v = wv; a.o = o; a.copy = o_copy; a.lse = lse;
     a.ko = kind_of(fout); a.fo = elem_fmt(fout); a.kc = kind_of(o_copy ? fcopy : fout); a.fc = elem_fmt(o_copy ? fcopy : fout);
     a.nbh = (int)p.nbh;
     a.flags = flags; a.vsrc = v; a.vb = d.vb; a.vl = d.vl; a.vh = d.vh; a.kv = kind_of(fkv); a.fv = elem_fmt(fkv);

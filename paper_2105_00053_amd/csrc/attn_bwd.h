@@ -40,6 +40,10 @@ struct AttnStats {
     ElemFmt fg, fo;
 };
 
+// Order of n tiles whose work falls with their number: the first half as it is, the second half backwards.  Where all workgroups are on the chip at once
+// a heavy and a light one share a compute unit; where they are not, the light ones come last but for the middle.
+__device__ __forceinline__ int at_light_last(int i, int n) { return i < (n + 1) / 2 ? i : n - 1 - (i - (n + 1) / 2); }
+
 // Eight lanes to a row, 32 rows to a workgroup.
 __global__ __launch_bounds__(256) void attn_stats_kernel(AttnStats a) {
     const AttnShape& s = a.s;
@@ -138,34 +142,34 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
     if (!live) return;
     const int64_t at = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + hk * s.G + (row - i * s.G)) * s.D;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int e = d * 32 + at_row(r, half);
-            if (e < s.D) store_value(a.dq, at + e, a.kout, a.fout, dq[d][r] * s.scale);
-        }
+    for (int d = 0; d < DB; ++d) {
+        dq[d] *= s.scale;
+        at_eights(dq[d], half, [&](int e, const float (&v)[8]) { at_store8(a.dq, at + d * 32 + e, s.D - d * 32 - e, a.kout, a.fout, v); });
+    }
 }
 
-// Four waves, 32 keys each; one block of 32 rows at a time.
+// 64 keys to a workgroup, two blocks of 32 rows at a time: of the four waves, two take each block of keys, one the even and one the odd blocks of
+// rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few; 128 keys to a
+// workgroup (32 to a wave) left the chip waiting for 16 of 256 workgroups (4 sequences of 2048, 64 elements a head: 250 us).
 template <int DB, bool TWO>
 __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd a) {
     constexpr int KS = 2 * DB, RUNS = 4 * KS;  // 1 KB runs of a block of rows: q, d_o, both transposed
-    __shared__ uint4 buf[2][RUNS * 64];
-    __shared__ __attribute__((aligned(16))) float stats[2][AT_STATS];
+    __shared__ uint4 buf[2][2][RUNS * 64];
+    __shared__ __attribute__((aligned(16))) float stats[2][2][AT_STATS];
     const AttnShape& s = a.s;
-    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
-    const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, odd = w >> 1;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = at_light_last(blockIdx.x / (unsigned)a.nbh, gridDim.x / (unsigned)a.nbh);
     const int b = bh / s.HKV, hk = bh - b * s.HKV, keys = at_keys(s, b), base = keys - s.LQ;
-    const int k0 = tile * 128, kw = k0 + w * 32, key = kw + (lane & 31);
+    const int k0 = tile * 64, kw = k0 + (w & 1) * 32, key = kw + (lane & 31);
     const float c = s.scale * 1.4426950408889634f;
     // the rows that see any of the workgroup's keys: from the position of its first key to the end of its last key's window
     const int i0 = k0 - base > 0 ? k0 - base : 0;
     int64_t i1 = s.LQ - 1;
-    if (s.window && k0 >= s.sinks && (int64_t)k0 + 126 + s.window - base < i1) i1 = (int64_t)k0 + 126 + s.window - base;
+    if (s.window && k0 >= s.sinks && (int64_t)k0 + 62 + s.window - base < i1) i1 = (int64_t)k0 + 62 + s.window - base;
     const int first = (int)((int64_t)i0 * s.G / 32), blocks = k0 >= keys || i0 > i1 ? 0 : (int)((i1 * s.G + s.G - 1) / 32) - first + 1;
 
     at_v8b kf[KS], vf[KS];
-    const int64_t mine = (int64_t)bh * s.kblocks + tile * 4 + w;
+    const int64_t mine = (int64_t)bh * s.kblocks + tile * 2 + (w & 1);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         kf[ks] = at_frag(a.k[(mine * KS + ks) * 64 + lane]);
@@ -173,12 +177,18 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
     }
     const int64_t rows0 = (int64_t)bh * s.qblocks;
     const uint4* const src = (w == 0 ? a.q : w == 1 ? a.g : w == 2 ? a.qt : a.gt) + rows0 * (KS * 64);
+    // a pair of blocks, of which the second may lie behind the last one that is wanted (it exists: the packed operands end at a multiple of 4)
     auto issue = [&](int n) {
-        const int64_t at = (int64_t)(first + n) * (KS * 64);
-        uint4* dst = buf[n & 1] + w * (KS * 64);
 #pragma unroll
-        for (int r = 0; r < KS; ++r) at_copy(src + at + r * 64, dst + r * 64, lane);
-        if (w == 0 && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + first + n) * AT_STATS), (uint4*)stats[n & 1], lane);
+        for (int x = 0; x < 2; ++x) {
+            const int blk = first + 2 * n + x;
+            if (2 * n + x >= blocks) break;
+            const int64_t at = (int64_t)blk * (KS * 64);
+            uint4* dst = buf[n & 1][x] + w * (KS * 64);
+#pragma unroll
+            for (int r = 0; r < KS; ++r) at_copy(src + at + r * 64, dst + r * 64, lane);
+            if (w == x && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + blk) * AT_STATS), (uint4*)stats[n & 1][x], lane);
+        }
     };
 
     at_v16f dk[DB], dv[DB];
@@ -188,12 +198,14 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
         dv[d] = at_zero();
     }
     if (blocks > 0) issue(0);
-    for (int n = 0; n < blocks; ++n) {
+    const int pairs = (blocks + 1) / 2;
+    for (int n = 0; n < pairs; ++n) {
         at_landed();
-        if (n + 1 < blocks) issue(n + 1);
-        const uint4* rb = buf[n & 1] + lane;
-        const float* st = stats[n & 1];
-        const int row0 = (first + n) * 32;
+        if (n + 1 < pairs) issue(n + 1);
+        if (2 * n + odd >= blocks) continue;
+        const uint4* rb = buf[n & 1][odd] + lane;
+        const float* st = stats[n & 1][odd];
+        const int row0 = (first + 2 * n + odd) * 32;
         const int p0 = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[64]));
         const int p1 = row0 + 31 < s.rows ? __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[95])) : base + s.LQ - 1;
         const int low0 = s.window ? p0 - s.window : -1, low1 = s.window ? p1 - s.window : -1;
@@ -240,8 +252,25 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
             }
         }
     }
+    // the waves of the even blocks finish dK, those of the odd ones dV
+    __syncthreads();
+    {
+        float* const mine = (float*)buf + (w & 1) * (DB * 2048) + lane;
+        float* const to = mine + (odd ? 0 : DB * 1024);
+        const float* const from = mine + (odd ? DB * 1024 : 0);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[(d * 16 + r) * 64] = odd ? dk[d][r] : dv[d][r];
+        __syncthreads();
+        // even + odd either way
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[d][r] = odd ? from[(d * 16 + r) * 64] + dv[d][r] : dk[d][r] + from[(d * 16 + r) * 64];
+    }
     bool flagged = false;
-    for (int n = lane; n < blocks; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
+    for (int n = lane; n < blocks && odd; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
     flagged = __any(flagged);
     if (key >= s.LK) return;
     AttnMarks marks = {};
@@ -259,17 +288,17 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
             }
         }
     const int64_t at = (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
+    void* const out = odd ? a.dv : a.dk;
+    const float up = odd ? 1.f : s.scale;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int e = d * 32 + at_row(r, half);
-            if (e >= s.D) continue;
-            store_value(a.dk, at + e, a.kout, a.fout, dk[d][r] * s.scale);
-            float v = dv[d][r];
-            if (flagged) v = marks.apply(16 * d + r, v);
-            store_value(a.dv, at + e, a.kout, a.fout, v);
+            dk[d][r] *= up;
+            if (flagged) dk[d][r] = marks.apply(16 * d + r, dk[d][r]);
         }
+        at_eights(dk[d], half, [&](int e, const float (&v)[8]) { at_store8(out, at + d * 32 + e, s.D - d * 32 - e, a.kout, a.fout, v); });
+    }
 }
 
 }  // namespace pnn

@@ -76,27 +76,28 @@ struct AttnPack {
     int B, HKV, D;
 };
 
-// 8 elements as bfloat16, exact for the formats accepted
-template <int K>
-__device__ __forceinline__ void at_load8(const void* p, int64_t at, int left, ElemFmt f, uint16_t (&o)[8]) {
-    typedef typename Raw<K>::T T;
-    const T* s = (const T*)p + at;
-    T raw[8];
-    if (left >= 8) {
-        __builtin_memcpy(raw, s, 8 * sizeof(T));
-    } else {
+// 8 elements as bfloat16, exact for the formats accepted; zeros in place of those beyond `left`
+__device__ __forceinline__ uint4 at_load8(const void* p, int64_t at, int left, int kind, ElemFmt f) {
+    Raw8 r;
+    load8(r, p, at, kind, left);
+    if (kind == KIND_BF16) return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    float v[8];
+    values8(v, r, kind, f);
+    uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) raw[i] = i < left ? s[i] : (T)0;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (uint16_t)(bits_of_f32(value_of<K>(raw[i], f)) >> 16);
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_perm(bits_of_f32(v[2 * i + 1]), bits_of_f32(v[2 * i]), 0x07060302u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
+
+// whether either half of a word is an infinity or a NaN
+__device__ __forceinline__ bool at_odd(uint32_t w) { return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u; }
 
 // One block of 32 rows of one operand to a workgroup, through LDS.
 template <int DB>
 __global__ __launch_bounds__(256) void attn_pack_kernel(AttnPack a) {
     constexpr int DP = 32 * DB, KS = 2 * DB;
     __shared__ uint16_t tile[32][DP + 2];
+    uint32_t* const words = (uint32_t*)&tile[0][0];
     const int n = blockIdx.z / a.B, b = blockIdx.z - n * a.B, hk = blockIdx.y, t = threadIdx.x;
     const AttnPackItem& p = a.item[n];
     const int blk = blockIdx.x;
@@ -105,19 +106,17 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnPack a) {
     for (int c = t; c < 32 * DP / 8; c += 256) {
         const int r = c / (DP / 8), d = (c - r * (DP / 8)) * 8;
         const int row = blk * 32 + r;
-        uint16_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        uint4 v = make_uint4(0, 0, 0, 0);
         if (row < p.rows && d < a.D) {
             const int i = row / p.G, g = row - i * p.G;
-            const int64_t at = b * p.sb + i * p.sl + (int64_t)(hk * p.G + g) * p.sh + d;
-            if (p.kind == KIND_POSIT_U8) at_load8<KIND_POSIT_U8>(p.src, at, a.D - d, p.f, v);
-            else if (p.kind == KIND_POSIT_U16) at_load8<KIND_POSIT_U16>(p.src, at, a.D - d, p.f, v);
-            else at_load8<KIND_BF16>(p.src, at, a.D - d, p.f, v);
+            v = at_load8(p.src, b * p.sb + i * p.sl + (int64_t)(hk * p.G + g) * p.sh + d, a.D - d, p.kind, p.f);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            tile[r][d + i] = v[i];
-            odd |= (v[i] & 0x7F80u) == 0x7F80u;
-        }
+        uint32_t* const to = words + r * (DP / 2 + 1) + d / 2;
+        to[0] = v.x;
+        to[1] = v.y;
+        to[2] = v.z;
+        to[3] = v.w;
+        odd |= at_odd(v.x) || at_odd(v.y) || at_odd(v.z) || at_odd(v.w);
     }
     const bool any = __syncthreads_or(odd);
     const int64_t bh = (int64_t)b * a.HKV + hk;
@@ -125,9 +124,7 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnPack a) {
     if (p.row_frags)
         for (int c = t; c < KS * 64; c += 256) {
             const int l = c & 63, r = l & 31, d = (c >> 6) * 16 + 8 * (l >> 5);
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)tile[r][d + 2 * i] | ((uint32_t)tile[r][d + 2 * i + 1] << 16);
+            const uint32_t* const w = words + r * (DP / 2 + 1) + d / 2;
             p.row_frags[(bh * p.blocks + blk) * KS * 64 + c] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     if (p.t_frags)
@@ -158,10 +155,53 @@ __device__ __forceinline__ at_v8b at_round(const at_v16f& v, int from) {
 }
 // what that rounding left, rounded in turn: together 16 bits
 __device__ __forceinline__ at_v8b at_rest(const at_v16f& v, int from, const at_v8b& hi) {
+    const at_v4u w = __builtin_bit_cast(at_v4u, hi);
     at_v8b o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (__bf16)(v[from + i] - (float)hi[i]);
+    for (int i = 0; i < 4; ++i) {
+        o[2 * i] = (__bf16)(v[from + 2 * i] - f32_of_bits(w[i] << 16));
+        o[2 * i + 1] = (__bf16)(v[from + 2 * i + 1] - f32_of_bits(w[i] & 0xFFFF0000u));
+    }
     return o;
+}
+
+// v.x of lanes 32 .. 63 and v.y of lanes 0 .. 31 change places
+__device__ __forceinline__ void at_swap_halves(float& x, float& y) {
+    typedef uint32_t v2 __attribute__((ext_vector_type(2)));
+    const v2 r = __builtin_amdgcn_permlane32_swap(bits_of_f32(x), bits_of_f32(y), false, false);
+    x = f32_of_bits(r.x);
+    y = f32_of_bits(r.y);
+}
+// the larger of a lane's value and that of the lane 32 away
+__device__ __forceinline__ float at_max_halves(float v) {
+    float w = v;
+    at_swap_halves(v, w);
+    return fmaxf(v, w);
+}
+// A block's 32 elements of the lane's row, 8 in a row at a time: f(first of them, values).  The halves of a wave hold the same rows; each takes
+// every other eight.
+template <class F>
+__device__ __forceinline__ void at_eights(const at_v16f& v, int half, F f) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = v[8 * q + i];
+            x[4 + i] = v[8 * q + 4 + i];
+            at_swap_halves(x[i], x[4 + i]);
+        }
+        f(8 * (2 * q + half), x);
+    }
+}
+__device__ __forceinline__ void at_store8(void* p, int64_t at, int left, int kind, ElemFmt f, const float (&v)[8]) {
+    if (left <= 0) return;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = v[i];
+    Raw8 r;
+    raw8<false>(r, w, kind, f);
+    store8(p, at, r, kind, left);
 }
 
 // The scale of the scores, as what exp2 takes: kept positive, so that the largest score has the largest exponent; its sign goes into q, and where it
@@ -179,18 +219,17 @@ __device__ __forceinline__ at_v8b at_scaled(uint4 v, float c) {
 
 // What infinities and NaN that a result's row sees make of it; the packed operand held zeros in their place.
 struct AttnMarks {
-    uint32_t pos[2], neg[2], nan[2];  // one bit a result register
+    uint64_t pos, neg, nan;  // one bit a result register
     __device__ __forceinline__ void add(int bit, float v) {
-        const uint32_t m = 1u << (bit & 31);
-        const bool hi = bit >= 32, inf = v - v != 0.f && v == v;
-        const uint32_t p = inf && v > 0.f ? m : 0u, n = inf && v < 0.f ? m : 0u, x = v != v ? m : 0u;
-        if (hi) { pos[1] |= p; neg[1] |= n; nan[1] |= x; }
-        else { pos[0] |= p; neg[0] |= n; nan[0] |= x; }
+        const uint64_t m = (uint64_t)1 << bit;
+        const bool inf = v - v != 0.f && v == v;
+        pos |= inf && v > 0.f ? m : 0;
+        neg |= inf && v < 0.f ? m : 0;
+        nan |= v != v ? m : 0;
     }
     __device__ __forceinline__ float apply(int bit, float v) const {
-        const int k = bit >> 5, sh = bit & 31;
-        const bool p = (pos[k] >> sh) & 1u, n = (neg[k] >> sh) & 1u;
-        if (((nan[k] >> sh) & 1u) || (p && n) || v != v) return f32_of_bits(0x7FC00000u);
+        const bool p = (pos >> bit) & 1u, n = (neg >> bit) & 1u;
+        if (((nan >> bit) & 1u) || (p && n) || v != v) return f32_of_bits(0x7FC00000u);
         return p ? f32_of_bits(0x7F800000u) : (n ? f32_of_bits(0xFF800000u) : v);
     }
 };

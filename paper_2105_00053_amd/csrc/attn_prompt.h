@@ -13,7 +13,11 @@ namespace pnn {
 
 struct AttnFwd {
     AttnShape s;
-    const uint4 *q, *k, *v;  // row fragments of q and k, transposed fragments of v
+    const void* q;        // read once, by the wave whose rows they are
+    int64_t qb, ql, qh;
+    int kq;
+    ElemFmt fq;
+    const uint4 *k, *v;   // row fragments, transposed fragments
     void *o, *copy;
     float* lse;
     int ko, kc;
@@ -67,10 +71,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
 
     float c = s.scale * 1.4426950408889634f;
     at_v8b q[KS];
-    {
-        const uint4* src = a.q + ((int64_t)bh * s.qblocks + tile * 4 + w) * (KS * 64) + lane;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = at_scaled(src[ks * 64], c);
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = ks * 16 + 8 * half;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (live && d < s.D) v = at_load8(a.q, b * a.qb + i * a.ql + (int64_t)(hk * s.G + (row - i * s.G)) * a.qh + d, s.D - d, a.kq, a.fq);
+        q[ks] = at_scaled(v, c);
     }
     c = at_scale(c);
 
@@ -118,7 +124,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[x][r]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+            mx = at_max_halves(mx) * c;
             if (__any(mx > m + 8.f)) {
                 const float m1 = fmaxf(m, mx), f = m1 == -inf ? 1.f : __builtin_amdgcn_exp2f(m - m1);
                 m = m1;
@@ -176,16 +182,18 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
     const int64_t at = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + h) * s.D;
     const float up = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
+    for (int d = 0; d < DB; ++d) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const int e = d * 32 + at_row(r, half);
-            if (e >= s.D) continue;
-            float v = o[d][r] * up;
-            if (flagged) v = marks.apply(16 * d + r, v);
-            store_value(a.o, at + e, a.ko, a.fo, v);
-            if (a.copy) store_value(a.copy, at + e, a.kc, a.fc, v);
+            o[d][r] *= up;
+            if (flagged) o[d][r] = marks.apply(16 * d + r, o[d][r]);
         }
+        at_eights(o[d], half, [&](int e, const float (&v)[8]) {
+            e += d * 32;
+            at_store8(a.o, at + e, s.D - e, a.ko, a.fo, v);
+            if (a.copy) at_store8(a.copy, at + e, s.D - e, a.kc, a.fc, v);
+        });
+    }
 }
 
 }  // namespace pnn

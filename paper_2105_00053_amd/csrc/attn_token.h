@@ -94,14 +94,8 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnToken a) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         const int d = ks * 16 + 8 * half;
-        uint16_t v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (live && d < s.D) {
-            const int64_t at = b * a.qb + i * a.ql + h * a.qh + d;
-            if (a.kq == KIND_POSIT_U8) at_load8<KIND_POSIT_U8>(a.q, at, s.D - d, a.fq, v);
-            else if (a.kq == KIND_POSIT_U16) at_load8<KIND_POSIT_U16>(a.q, at, s.D - d, a.fq, v);
-            else at_load8<KIND_BF16>(a.q, at, s.D - d, a.fq, v);
-        }
-        uint4 u = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (live && d < s.D) u = at_load8(a.q, b * a.qb + i * a.ql + h * a.qh + d, s.D - d, a.kq, a.fq);
         q[ks] = at_scaled(u, c);
     }
     c = at_scale(c);
@@ -110,7 +104,7 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnToken a) {
     const T* const ksrc = (const T*)a.k + b * a.kb + hk * a.kh;
     const T* const vsrc = (const T*)a.v + b * a.vb + hk * a.vh;
     const int keys = base + s.LQ;
-    auto load = [&](int n, AttnRaw<K, KS>& r) {
+    auto load_keys = [&](int n, AttnRaw<K, KS>& r) {
         const int key0 = tiles.at(n) * 32;
         {
             const int key = key0 + col;
@@ -118,6 +112,9 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnToken a) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) at_words<T, 8>(src + ks * 16 + 8 * half, s.D - (ks * 16 + 8 * half), r.k[ks]);
         }
+    };
+    auto load_values = [&](int n, AttnRaw<K, KS>& r) {
+        const int key0 = tiles.at(n) * 32;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int key = key0 + (e >> 3) * 16 + at_row(e & 7, half);
@@ -157,10 +154,19 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnToken a) {
     for (int x = 0; x < 4; ++x) o[x] = at_zero();
     uint32_t flagged = 0;
     AttnRaw<K, KS> raw;
-    if (begin + w < end) load(begin + w, raw);
+    // the next tile is on its way while one is worked on; of 16-bit elements only its keys, for which there are registers
+    constexpr bool AHEAD = sizeof(T) == 1;
+    if (begin + w < end) {
+        load_keys(begin + w, raw);
+        if (AHEAD) load_values(begin + w, raw);
+    }
     for (int n = begin + w; n < end; n += 4) {
+        if (!AHEAD) load_values(n, raw);
         const AttnRaw<K, KS> cur = raw;
-        if (n + 4 < end) load(n + 4, raw);
+        if (n + 4 < end) {
+            load_keys(n + 4, raw);
+            if (AHEAD) load_values(n + 4, raw);
+        }
         const int key0 = tiles.at(n) * 32;
         at_v16f sc = at_zero();
 #pragma unroll
@@ -175,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnToken a) {
         float mx = sc[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c;
+        mx = at_max_halves(mx) * c;
         if (__any(mx > m + 8.f)) {
             const float m1 = fmaxf(m, mx), f = m1 == -inf ? 1.f : __builtin_amdgcn_exp2f(m - m1);
             m = m1;

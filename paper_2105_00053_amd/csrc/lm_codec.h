@@ -141,20 +141,31 @@ PNN_HD void store_value(void* p, int64_t i, int kind, ElemFmt f, float v) {
     }
 
 // ---- eight elements in a row, of a kind known at run time (uniform: the branches are the wave's) ----
-// As they lie in memory; alignment is the element type's (wide loads and stores take any address here).
+// As they lie in memory, in a vector rather than an array: an array whose elements are taken under several conditions ends up in scratch
+// memory.  Alignment is the element type's (wide loads and stores take any address here).
+typedef uint32_t words8 __attribute__((ext_vector_type(8)));
+typedef uint32_t words2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t words4_any __attribute__((ext_vector_type(4), aligned(1)));
 struct Raw8 {
-    uint32_t w[8];
+    words8 w;
 };
 
 __device__ __forceinline__ void load8(Raw8& r, const void* p, int64_t i, int kind, int left) {
     if (left >= 8) {
-        if (kind == KIND_POSIT_U8) __builtin_memcpy(r.w, (const uint8_t*)p + i, 8);
-        else if (kind == KIND_F32) __builtin_memcpy(r.w, (const uint8_t*)p + 4 * i, 32);
-        else __builtin_memcpy(r.w, (const uint8_t*)p + 2 * i, 16);
+        if (kind == KIND_POSIT_U8) {
+            const words2_any v = *(const words2_any*)((const uint8_t*)p + i);
+            r.w.lo.lo = v;
+        } else if (kind == KIND_F32) {
+            const words4_any *const q = (const words4_any*)((const uint8_t*)p + 4 * i), v0 = q[0], v1 = q[1];
+            r.w.lo = v0;
+            r.w.hi = v1;
+        } else {
+            const words4_any v = *(const words4_any*)((const uint8_t*)p + 2 * i);
+            r.w.lo = v;
+        }
         return;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r.w[e] = 0;
+    r.w = (words8)(0u);
     if (kind == KIND_POSIT_U8) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -251,17 +262,29 @@ __device__ __forceinline__ void raw8(Raw8& r, float (&v)[8], int kind, ElemFmt f
 
 __device__ __forceinline__ void store8(void* p, int64_t i, const Raw8& r, int kind, int left) {
     if (left >= 8) {
-        if (kind == KIND_POSIT_U8) __builtin_memcpy((uint8_t*)p + i, r.w, 8);
-        else if (kind == KIND_F32) __builtin_memcpy((uint8_t*)p + 4 * i, r.w, 32);
-        else __builtin_memcpy((uint8_t*)p + 2 * i, r.w, 16);
+        if (kind == KIND_POSIT_U8) {
+            *(words2_any*)((uint8_t*)p + i) = r.w.lo.lo;
+        } else if (kind == KIND_F32) {
+            words4_any* const q = (words4_any*)((uint8_t*)p + 4 * i);
+            q[0] = r.w.lo;
+            q[1] = r.w.hi;
+        } else {
+            *(words4_any*)((uint8_t*)p + 2 * i) = r.w.lo;
+        }
         return;
     }
+    if (kind == KIND_POSIT_U8) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if (e >= left) continue;
-        if (kind == KIND_POSIT_U8) ((uint8_t*)p)[i + e] = (uint8_t)(r.w[e / 4] >> (8 * (e & 3)));
-        else if (kind == KIND_F32) ((uint32_t*)p)[i + e] = r.w[e];
-        else ((uint16_t*)p)[i + e] = (uint16_t)(r.w[e / 2] >> (16 * (e & 1)));
+        for (int e = 0; e < 8; ++e)
+            if (e < left) ((uint8_t*)p)[i + e] = (uint8_t)(r.w[e / 4] >> (8 * (e & 3)));
+    } else if (kind == KIND_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) ((uint32_t*)p)[i + e] = r.w[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) ((uint16_t*)p)[i + e] = (uint16_t)(r.w[e / 2] >> (16 * (e & 1)));
     }
 }
 
