@@ -109,7 +109,7 @@ void launch_fwd(hipStream_t st, const Plan& p, const AttnFwd& a) {
 template <int DB, bool TWO>
 void launch_bwd_of(hipStream_t st, const Plan& p, const AttnBwd& a) {
     if (p.s.LQ > 0) hipLaunchKernelGGL((attn_dq_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.qblocks / 4))), dim3(256), 0, st, a);
-    if (p.s.LK > 0) hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 2))), dim3(256), 0, st, a);
+    if (p.s.LK > 0) hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 2))), dim3(128 * at_parallel(DB)), 0, st, a);
 }
 
 template <bool TWO>

@@ -148,16 +148,18 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
     }
 }
 
-// 64 keys to a workgroup, two blocks of 32 rows at a time: of the four waves, two take each block of keys, one the even and one the odd blocks of
-// rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few; 128 keys to a
-// workgroup (32 to a wave) left the chip waiting for 16 of 256 workgroups (4 sequences of 2048, 64 elements a head: 250 us).
+// 64 keys to a workgroup, NP blocks of 32 rows at a time: of its 2 NP waves, NP take each block of 32 keys, each with every NP-th block of
+// rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few, so the length of the longest
+// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four see below.
+constexpr int at_parallel(int db) { return db <= 2 ? 4 : 2; }  // what LDS (128 KB) holds of two stages
+
 template <int DB, bool TWO>
-__global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd a) {
-    constexpr int KS = 2 * DB, RUNS = 4 * KS;  // 1 KB runs of a block of rows: q, d_o, both transposed
-    __shared__ uint4 buf[2][2][RUNS * 64];
-    __shared__ __attribute__((aligned(16))) float stats[2][2][AT_STATS];
+__global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd a) {
+    constexpr int KS = 2 * DB, NP = at_parallel(DB), RUNS = 4 * KS;  // 1 KB runs of a block of rows: q, d_o, both transposed
+    __shared__ uint4 buf[2][NP][RUNS * 64];
+    __shared__ __attribute__((aligned(16))) float stats[2][NP][AT_STATS];
     const AttnShape& s = a.s;
-    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, odd = w >> 1;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, turn = w >> 1;
     const int bh = blockIdx.x % (unsigned)a.nbh, tile = at_light_last(blockIdx.x / (unsigned)a.nbh, gridDim.x / (unsigned)a.nbh);
     const int b = bh / s.HKV, hk = bh - b * s.HKV, keys = at_keys(s, b), base = keys - s.LQ;
     const int k0 = tile * 64, kw = k0 + (w & 1) * 32, key = kw + (lane & 31);
@@ -176,19 +178,21 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
         vf[ks] = at_frag(a.v[(mine * KS + ks) * 64 + lane]);
     }
     const int64_t rows0 = (int64_t)bh * s.qblocks;
-    const uint4* const src = (w == 0 ? a.q : w == 1 ? a.g : w == 2 ? a.qt : a.gt) + rows0 * (KS * 64);
-    // a pair of blocks, of which the second may lie behind the last one that is wanted (it exists: the packed operands end at a multiple of 4)
+    // Blocks from the last one down: that is where the rows of all of a sequence's workgroups end, which so read the same blocks at about
+    // the same time (4 MB of packed rows a sequence and head group do not fit an L2).  Each wave copies two of its own block's four operands.
+    const int last = first + blocks - 1;
+    const uint4* const src[2] = {((w & 1) ? a.g : a.q) + rows0 * (KS * 64), ((w & 1) ? a.gt : a.qt) + rows0 * (KS * 64)};
     auto issue = [&](int n) {
+        const int blk = last - NP * n - turn;
+        if (NP * n + turn >= blocks) return;
+        const int64_t at = (int64_t)blk * (KS * 64);
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            const int blk = first + 2 * n + x;
-            if (2 * n + x >= blocks) break;
-            const int64_t at = (int64_t)blk * (KS * 64);
-            uint4* dst = buf[n & 1][x] + w * (KS * 64);
+            uint4* dst = buf[n & 1][turn] + (2 * x + (w & 1)) * (KS * 64);
 #pragma unroll
-            for (int r = 0; r < KS; ++r) at_copy(src + at + r * 64, dst + r * 64, lane);
-            if (w == x && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + blk) * AT_STATS), (uint4*)stats[n & 1][x], lane);
+            for (int r = 0; r < KS; ++r) at_copy(src[x] + at + r * 64, dst + r * 64, lane);
         }
+        if ((w & 1) == 0 && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + blk) * AT_STATS), (uint4*)stats[n & 1][turn], lane);
     };
 
     at_v16f dk[DB], dv[DB];
@@ -198,14 +202,14 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
         dv[d] = at_zero();
     }
     if (blocks > 0) issue(0);
-    const int pairs = (blocks + 1) / 2;
-    for (int n = 0; n < pairs; ++n) {
+    const int rounds = (blocks + NP - 1) / NP;
+    for (int n = 0; n < rounds; ++n) {
         at_landed();
-        if (n + 1 < pairs) issue(n + 1);
-        if (2 * n + odd >= blocks) continue;
-        const uint4* rb = buf[n & 1][odd] + lane;
-        const float* st = stats[n & 1][odd];
-        const int row0 = (first + 2 * n + odd) * 32;
+        if (n + 1 < rounds) issue(n + 1);
+        if (NP * n + turn >= blocks) continue;
+        const uint4* rb = buf[n & 1][turn] + lane;
+        const float* st = stats[n & 1][turn];
+        const int row0 = (last - NP * n - turn) * 32;
         const int p0 = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[64]));
         const int p1 = row0 + 31 < s.rows ? __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[95])) : base + s.LQ - 1;
         const int low0 = s.window ? p0 - s.window : -1, low1 = s.window ? p1 - s.window : -1;
@@ -252,25 +256,34 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
             }
         }
     }
-    // the waves of the even blocks finish dK, those of the odd ones dV
+    // turn 0 finishes dK, turn 1 dV
     __syncthreads();
     {
-        float* const mine = (float*)buf + (w & 1) * (DB * 2048) + lane;
-        float* const to = mine + (odd ? 0 : DB * 1024);
-        const float* const from = mine + (odd ? DB * 1024 : 0);
+        constexpr int PART = DB * 1024;  // floats of one wave's dK or dV
+        float* const mine = (float*)buf + (w & 1) * (NP * 2 * PART) + lane;
+        auto slot = [&](int of, int what, int d, int r) -> float& { return mine[(of * 2 + what) * PART + (d * 16 + r) * 64]; };
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) to[(d * 16 + r) * 64] = odd ? dk[d][r] : dv[d][r];
+            for (int r = 0; r < 16; ++r) {
+                if (turn != 0) slot(turn, 0, d, r) = dk[d][r];
+                if (turn != 1) slot(turn, 1, d, r) = dv[d][r];
+            }
         __syncthreads();
-        // even + odd either way
+        if (turn > 1) return;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dk[d][r] = odd ? from[(d * 16 + r) * 64] + dv[d][r] : dk[d][r] + from[(d * 16 + r) * 64];
+            for (int r = 0; r < 16; ++r) {
+                float v = turn == 0 ? dk[d][r] : slot(0, 1, d, r);
+                v += turn == 0 ? slot(1, 0, d, r) : dv[d][r];
+#pragma unroll
+                for (int x = 2; x < NP; ++x) v += slot(x, turn, d, r);
+                dk[d][r] = v;
+            }
     }
     bool flagged = false;
-    for (int n = lane; n < blocks && odd; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
+    for (int n = lane; n < blocks && turn == 1; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
     flagged = __any(flagged);
     if (key >= s.LK) return;
     AttnMarks marks = {};
@@ -288,8 +301,8 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd 
             }
         }
     const int64_t at = (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
-    void* const out = odd ? a.dv : a.dk;
-    const float up = odd ? 1.f : s.scale;
+    void* const out = turn ? a.dv : a.dk;
+    const float up = turn ? 1.f : s.scale;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
 #pragma unroll
