@@ -164,7 +164,7 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     discard_stale_hip_error();
     Plan p = make_plan(d);
     p.s.lens = lens;
-    const bool two = fout != PNN_BF16 || (o_copy && fcopy != PNN_BF16);
+    const bool two = fout != PNN_BF16;  // the probabilities to 16 bits
     const TokenPlan tp = token_plan(d);
     if (tp.use) {
         AttnToken a = {};

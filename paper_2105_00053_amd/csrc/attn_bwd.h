@@ -40,10 +40,6 @@ struct AttnStats {
     ElemFmt fg, fo;
 };
 
-// Order of n tiles whose work falls with their number: the first half as it is, the second half backwards.  Where all workgroups are on the chip at once
-// a heavy and a light one share a compute unit; where they are not, the light ones come last but for the middle.
-__device__ __forceinline__ int at_light_last(int i, int n) { return i < (n + 1) / 2 ? i : n - 1 - (i - (n + 1) / 2); }
-
 // Eight lanes to a row, 32 rows to a workgroup.
 __global__ __launch_bounds__(256) void attn_stats_kernel(AttnStats a) {
     const AttnShape& s = a.s;
@@ -71,7 +67,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
     __shared__ uint4 buf[2][RUNS * 64];
     const AttnShape& s = a.s;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
-    const int bh = blockIdx.x % (unsigned)a.nbh, tile = gridDim.x / (unsigned)a.nbh - 1 - blockIdx.x / (unsigned)a.nbh;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = gridDim.x / (unsigned)a.nbh - 1 - at_snake(blockIdx.x / (unsigned)a.nbh, gridDim.x / (unsigned)a.nbh, a.nbh);
     const int b = bh / s.HKV, hk = bh - b * s.HKV, base = at_keys(s, b) - s.LQ;
     const int r0 = tile * 128, rw = r0 + w * 32, row = rw + (lane & 31);
     const int last = (r0 + 128 < s.rows ? r0 + 128 : s.rows) - 1;
@@ -116,9 +112,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
         const uint4* kb = buf[n & 1] + lane;
         at_v16f sc = at_zero(), dp = at_zero();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sc = at_mfma(at_frag(kb[ks * 64]), q[ks], sc);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = at_mfma(at_frag(kb[(KS + ks) * 64]), g[ks], dp);
+        for (int ks = 0; ks < KS; ++ks) {
+            sc = at_mfma(at_frag(kb[ks * 64]), q[ks], sc);
+            dp = at_mfma(at_frag(kb[(KS + ks) * 64]), g[ks], dp);
+        }
         const bool whole = key0 + 31 <= wp0 && (key0 > wlow1 || key0 + 31 < s.sinks);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -lse)) * (dp[r] - dd);
@@ -160,7 +157,7 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
     __shared__ __attribute__((aligned(16))) float stats[2][NP][AT_STATS];
     const AttnShape& s = a.s;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, turn = w >> 1;
-    const int bh = blockIdx.x % (unsigned)a.nbh, tile = at_light_last(blockIdx.x / (unsigned)a.nbh, gridDim.x / (unsigned)a.nbh);
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh;
     const int b = bh / s.HKV, hk = bh - b * s.HKV, keys = at_keys(s, b), base = keys - s.LQ;
     const int k0 = tile * 64, kw = k0 + (w & 1) * 32, key = kw + (lane & 31);
     const float c = s.scale * 1.4426950408889634f;
@@ -203,23 +200,31 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
     }
     if (blocks > 0) issue(0);
     const int rounds = (blocks + NP - 1) / NP;
+    // row / G of the wave's block, kept up to date without a division a round
+    int quot = (last - turn) * 32 / s.G, rem = (last - turn) * 32 - quot * s.G;
+    const int reach = (31 + s.G - 1) / s.G;
     for (int n = 0; n < rounds; ++n) {
         at_landed();
         if (n + 1 < rounds) issue(n + 1);
         if (NP * n + turn >= blocks) continue;
         const uint4* rb = buf[n & 1][turn] + lane;
         const float* st = stats[n & 1][turn];
-        const int row0 = (last - NP * n - turn) * 32;
-        const int p0 = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[64]));
-        const int p1 = row0 + 31 < s.rows ? __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, st[95])) : base + s.LQ - 1;
+        const int row0 = (last - NP * n - turn) * 32, p0 = base + quot, p1 = p0 + reach;  // p1: the last row's position or more
+        quot -= NP * 32 / s.G;
+        rem -= NP * 32 % s.G;
+        if (rem < 0) {
+            rem += s.G;
+            --quot;
+        }
         const int low0 = s.window ? p0 - s.window : -1, low1 = s.window ? p1 - s.window : -1;
         if (!(kw <= p1 && (kw + 31 > low0 || kw < s.sinks))) continue;
         const bool whole = kw + 31 <= p0 && (kw > low1 || kw + 31 < s.sinks) && row0 + 31 < s.rows;
         at_v16f sc = at_zero(), dp = at_zero();
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sc = at_mfma(at_frag(rb[ks * 64]), kf[ks], sc);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = at_mfma(at_frag(rb[(KS + ks) * 64]), vf[ks], dp);
+        for (int ks = 0; ks < KS; ++ks) {
+            sc = at_mfma(at_frag(rb[ks * 64]), kf[ks], sc);
+            dp = at_mfma(at_frag(rb[(KS + ks) * 64]), vf[ks], dp);
+        }
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -st[at_row(r, half)]));
         if (!whole) {

@@ -44,6 +44,19 @@ __device__ __forceinline__ void at_landed() {
 }
 
 // Positions, rows and blocks of one sequence fit 32 bits; offsets into tensors do not.
+// Positions, rows and blocks of one sequence fit 32 bits; offsets into tensors do not.
+// N matrix instructions with an LDS read each: AHEAD reads in front, then one read for each instruction.
+template <int N, int AHEAD>
+__device__ __forceinline__ void at_order() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int i = 0; i < N - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 struct AttnShape {
     int LQ, LK;
     int window, sinks;      // window 0: none, which any of LK keys or more is; sinks at most LK
@@ -60,6 +73,13 @@ __device__ __forceinline__ int at_keys(const AttnShape& s, int64_t b) {
 }
 // whether a query at position p sees a key; low = the last position in front of its window
 __device__ __forceinline__ bool at_sees(const AttnShape& s, int p, int low, int key) { return key <= p && (key > low || key < s.sinks); }
+
+// Order of n tiles whose work falls with their number, for nbh heads each: back and forth over as many tiles as fill the chip's 256 compute
+// units once, so that the workgroups that share a unit have about the same work together.
+__device__ __forceinline__ int at_snake(int i, int n, int nbh) {
+    const int lap = nbh < 256 ? 256 / nbh : 1, turn = i / lap, first = turn * lap, size = n - first < lap ? n - first : lap;
+    return (turn & 1) ? first + size - 1 - (i - first) : i;
+}
 
 struct AttnPackItem {
     const void* src;

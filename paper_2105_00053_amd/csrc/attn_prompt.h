@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
     const AttnShape& s = a.s;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5;
     // the last rows first: with a causal mask they see most
-    const int bh = blockIdx.x % (unsigned)a.nbh, tile = gridDim.x / (unsigned)a.nbh - 1 - blockIdx.x / (unsigned)a.nbh;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = gridDim.x / (unsigned)a.nbh - 1 - at_snake(blockIdx.x / (unsigned)a.nbh, gridDim.x / (unsigned)a.nbh, a.nbh);
     const int b = bh / s.HKV, hk = bh - b * s.HKV, base = at_keys(s, b) - s.LQ;
     const int r0 = tile * 128, rw = r0 + w * 32, row = rw + (lane & 31);
     const int last = (r0 + 128 < s.rows ? r0 + 128 : s.rows) - 1;
