@@ -81,8 +81,8 @@ __device__ __forceinline__ void norm_reduce(int T, float* part, uint32_t* partu,
     }
 }
 
-// Rows of up to 8192 elements, 8 to a thread: read once, with the next row's loads in flight, written once.  T threads (a power of two
-// of waves) to a row; the weights are decoded once for all rows of a workgroup.  KR < 0: no residual.
+// Rows of up to 8192 elements, 8 to a thread: read once, with the next row's loads in flight, written once.  T threads (whole
+// waves) to a row; the weights are decoded once for all rows of a workgroup.  KR < 0: no residual.
 template <int KX, int KR>
 __global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T) {
     __shared__ float part[32];
@@ -361,18 +361,19 @@ __global__ __launch_bounds__(256) void scale_rows_kernel(const void* x, int64_t 
     store8(y, r * ldy + j, raw, ky, left);
 }
 
-// Threads to a row, threads and number of workgroups.  Rows beyond 8 elements a thread of the largest workgroup have kernels of their own.
+// Threads to a row (whole waves of them), threads and number of workgroups.  Rows beyond 8 elements a thread of the largest workgroup have kernels
+// of their own.
 struct NormPlan {
     bool rows;
     int T, threads;
     unsigned groups;
 };
 inline NormPlan norm_plan(int64_t rows, int64_t cols) {
-    NormPlan p = {cols <= 8192, 64, 256, 0};
-    while (p.T * 8 < cols && p.T < 1024) p.T *= 2;
-    if (p.threads < p.T) p.threads = p.T;
+    NormPlan p = {cols <= 8192, 1024, 1024, 0};
+    if (p.rows) p.T = (int)((cols + 511) / 512) * 64;
+    p.threads = p.T == 64 || p.T == 128 ? 256 : p.T;
     // as many workgroups as the chip holds, 2048 threads to a compute unit; each walks over rows
-    const int64_t want = (rows + p.threads / p.T - 1) / (p.threads / p.T), most = 256 * 2048 / p.threads;
+    const int64_t want = (rows + p.threads / p.T - 1) / (p.threads / p.T), most = 256 * (2048 / p.threads);
     p.groups = (unsigned)(want < most ? want : most);
     return p;
 }

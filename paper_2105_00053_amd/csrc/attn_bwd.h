@@ -49,7 +49,16 @@ __global__ __launch_bounds__(256) void attn_stats_kernel(AttnStats a) {
     float d = 0.f;
     if (live) {
         const int64_t ga = b * a.gb + i * a.gl + h * a.gh, oa = (((int64_t)b * s.LQ + i) * HQ + h) * s.D;
-        for (int e = t & 7; e < s.D; e += 8) d = fmaf(load_value(a.g, ga + e, a.kg, a.fg), load_value(a.o, oa + e, a.ko, a.fo), d);
+        for (int e = (t & 7) * 8; e < s.D; e += 64) {
+            Raw8 rg, ro;
+            load8(rg, a.g, ga + e, a.kg, s.D - e);
+            load8(ro, a.o, oa + e, a.ko, s.D - e);
+            float g[8], o[8];
+            values8(g, rg, a.kg, a.fg);
+            values8(o, ro, a.ko, a.fo);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) d = fmaf(g[x], o[x], d);
+        }
     }
 #pragma unroll
     for (int m = 4; m >= 1; m >>= 1) d += __shfl_xor(d, m, 64);
