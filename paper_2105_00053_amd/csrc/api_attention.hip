@@ -42,16 +42,16 @@ struct Plan {
 // prompt kernel reads a packed copy and has a workgroup to 128 rows.
 struct TokenPlan {
     bool use;
-    int blocks, parts, tiles;  // row blocks of 32, parts of the keys, tiles of 32 keys in a part
+    int blocks, parts, tiles;  // row blocks of 16, parts of the keys, tiles of 32 keys in a part
     int64_t bytes;
 };
 
 TokenPlan token_plan(const pnn_attention_desc& d) {
     TokenPlan t = {};
     const int64_t g = d.HKV ? d.HQ / d.HKV : 1, rows = d.LQ * g;
-    t.use = rows <= 32 || (rows <= 128 && d.LK >= 4 * rows);
+    t.use = rows <= 16 || (rows <= 64 && d.LK >= 8 * rows);
     if (!t.use) return t;
-    t.blocks = (int)((rows + 31) / 32);
+    t.blocks = (int)((rows + 15) / 16);
     int64_t keys = d.LK;
     if (d.window > 0 && d.window + d.LQ + d.sinks + 64 < keys) keys = d.window + d.LQ + d.sinks + 64;
     const int64_t all = (keys + 31) / 32 + 1, groups = d.B * d.HKV * t.blocks;
@@ -62,7 +62,7 @@ TokenPlan token_plan(const pnn_attention_desc& d) {
     t.tiles = (int)((all + parts - 1) / parts);
     t.tiles = (t.tiles + 3) / 4 * 4;
     t.parts = (int)((all + t.tiles - 1) / t.tiles);
-    t.bytes = t.parts > 1 ? groups * t.parts * 32 * (d.D + 2) * 4 : 0;
+    t.bytes = t.parts > 1 ? groups * t.parts * 16 * (d.D + 2) * 4 : 0;
     return t;
 }
 

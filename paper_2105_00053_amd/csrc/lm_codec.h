@@ -166,18 +166,31 @@ __device__ __forceinline__ void load8(Raw8& r, const void* p, int64_t i, int kin
         return;
     }
     r.w = (words8)(0u);
+    if (left <= 0) return;
+    // the end of a row: all eight loads at once, of the first element in place of those behind the end (one load after the other, each behind a
+    // condition, made a row of 5119 wait for seven memory latencies)
+    uint32_t v[8];
     if (kind == KIND_POSIT_U8) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) r.w[e / 4] |= (uint32_t)((const uint8_t*)p)[i + e] << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e) v[e] = ((const uint8_t*)p)[i + (e < left ? e : 0)];
     } else if (kind == KIND_F32) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) r.w[e] = ((const uint32_t*)p)[i + e];
+        for (int e = 0; e < 8; ++e) v[e] = ((const uint32_t*)p)[i + (e < left ? e : 0)];
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < left) r.w[e / 2] |= (uint32_t)((const uint16_t*)p)[i + e] << (16 * (e & 1));
+        for (int e = 0; e < 8; ++e) v[e] = ((const uint16_t*)p)[i + (e < left ? e : 0)];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? v[e] : 0u;
+    if (kind == KIND_POSIT_U8) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) r.w[e] = v[4 * e] | v[4 * e + 1] << 8 | v[4 * e + 2] << 16 | v[4 * e + 3] << 24;
+    } else if (kind == KIND_F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.w[e] = v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.w[e] = v[2 * e] | v[2 * e + 1] << 16;
     }
 }
 
