@@ -124,9 +124,12 @@ void launch_bwd(hipStream_t st, const Plan& p, const AttnBwd& a) {
 
 template <int K>
 void launch_token(hipStream_t st, int db, bool two, const dim3& grid, const AttnToken& a) {
-#define PNN_TOKEN(DB)                                                                                             \
-    if (two) hipLaunchKernelGGL((attn_token_kernel<K, DB, true>), grid, dim3(256), 0, st, a);   \
-    else hipLaunchKernelGGL((attn_token_kernel<K, DB, false>), grid, dim3(256), 0, st, a);
+    const bool whole = a.s.D % 8 == 0;
+#define PNN_TOKEN(DB)                                                                                                    \
+    if (two && whole) hipLaunchKernelGGL((attn_token_kernel<K, DB, true, true>), grid, dim3(256), 0, st, a);             \
+    else if (two) hipLaunchKernelGGL((attn_token_kernel<K, DB, true, false>), grid, dim3(256), 0, st, a);                \
+    else if (whole) hipLaunchKernelGGL((attn_token_kernel<K, DB, false, true>), grid, dim3(256), 0, st, a);              \
+    else hipLaunchKernelGGL((attn_token_kernel<K, DB, false, false>), grid, dim3(256), 0, st, a);
     switch (db) {
         case 1: PNN_TOKEN(1) break;
         case 2: PNN_TOKEN(2) break;

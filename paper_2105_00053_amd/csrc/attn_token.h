@@ -62,7 +62,9 @@ __device__ __forceinline__ void at_words(const T* src, int left, uint32_t (&o)[N
     }
 }
 
-template <int K, int DB, bool TWO>
+// WHOLE: heads of a multiple of 8 elements, so that a vector lies inside one or outside; those outside are read from the head's start and, of keys,
+// taken as zero (of values they go to elements that do not exist).
+template <int K, int DB, bool TWO, bool WHOLE>
 __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void attn_token_kernel(AttnToken a) {
     constexpr int KS = DB, NV = DB <= 2 ? 4 : 8;
     __shared__ uint32_t smem[8192];  // the table, then what the waves join through
@@ -94,7 +96,11 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
             const int key = key0 + 16 * x + col;
             const T* src = ksrc + (int64_t)(key < keys ? key : keys - 1) * a.kl;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) at_words<T, 8>(src + ks * 32 + 8 * quarter, s.D - (ks * 32 + 8 * quarter), r.k[x][ks]);
+            for (int ks = 0; ks < KS; ++ks) {
+                const int d = ks * 32 + 8 * quarter;
+                if (WHOLE) __builtin_memcpy(r.k[x][ks], src + (d < s.D ? d : 0), 8 * sizeof(T));
+                else at_words<T, 8>(src + d, s.D - d, r.k[x][ks]);
+            }
         }
     };
     auto load_values = [&](int n, R& r) {
@@ -102,7 +108,9 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int key = key0 + key_of(e);
-            at_words<T, NV>(vsrc + (int64_t)(key < keys ? key : keys - 1) * a.vl + NV * col, s.D - NV * col, r.v[e]);
+            const T* src = vsrc + (int64_t)(key < keys ? key : keys - 1) * a.vl;
+            if (WHOLE) __builtin_memcpy(r.v[e], src + (NV * col < s.D ? NV * col : 0), NV * sizeof(T));
+            else at_words<T, NV>(src + NV * col, s.D - NV * col, r.v[e]);
         }
     };
     // the next tile is on its way while one is worked on; of 16-bit elements only its keys, for which there are registers
@@ -181,7 +189,9 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const uint32_t* e = cur.k[x][ks];
-                acc = at_mfma16(at_frag(make_uint4(pair(e, 0, e, 1, false), pair(e, 2, e, 3, false), pair(e, 4, e, 5, false), pair(e, 6, e, 7, false))), q[ks], acc);
+                uint4 u = make_uint4(pair(e, 0, e, 1, false), pair(e, 2, e, 3, false), pair(e, 4, e, 5, false), pair(e, 6, e, 7, false));
+                if (WHOLE && ks == KS - 1) u = ks * 32 + 8 * quarter < s.D ? u : make_uint4(0, 0, 0, 0);
+                acc = at_mfma16(at_frag(u), q[ks], acc);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) sc[4 * x + r] = acc[r];
