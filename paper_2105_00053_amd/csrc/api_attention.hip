@@ -55,9 +55,11 @@ TokenPlan token_plan(const pnn_attention_desc& d) {
     int64_t keys = d.LK;
     if (d.window > 0 && d.window + d.LQ + d.sinks + 64 < keys) keys = d.window + d.LQ + d.sinks + 64;
     const int64_t all = (keys + 31) / 32 + 1, groups = d.B * d.HKV * t.blocks;
-    // four workgroups to a compute unit, at least four tiles (one to a wave) in a part; short caches stay whole, the second kernel costs more
-    int64_t parts = groups > 0 ? (1024 + groups - 1) / groups : 1;
+    // Two workgroups to a compute unit, at least a tile to each of their waves; short caches stay whole, the second kernel costs more.  48 sequences of
+    // 4096 keys, 8 heads of 128: 112 us in 2 parts, 110 in 3, 124 in 4; 8 sequences of 8192: 47 in 8 parts, 52 in 16, 59 in 24.
+    int64_t parts = groups > 0 ? (512 + groups - 1) / groups : 1;
     if (parts > all / 4) parts = all / 4;
+    if (parts > AT_MOST_PARTS) parts = AT_MOST_PARTS;
     if (parts < 1 || all <= 16) parts = 1;
     t.tiles = (int)((all + parts - 1) / parts);
     t.tiles = (t.tiles + 3) / 4 * 4;

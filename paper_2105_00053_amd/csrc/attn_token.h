@@ -21,6 +21,7 @@ typedef float at_v4f __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ at_v4f at_mfma16(at_v8b a, at_v8b b, at_v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 constexpr int AT_TOKEN_ROWS = 16;
+constexpr int AT_MOST_PARTS = 256;  // workgroups to a row block's keys, what the second kernel holds weights of
 
 struct AttnToken {
     AttnShape s;
@@ -308,30 +309,52 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
 
 // Parts of a row joined, one row to a workgroup and an element to a thread.
 __global__ __launch_bounds__(128) void attn_join_kernel(AttnToken a) {
+    __shared__ float weight[AT_MOST_PARTS];
+    __shared__ float half_max[2], half_sum[2];
     const AttnShape& s = a.s;
-    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, d = threadIdx.x, rr = row & 15;
+    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x, rr = row & 15;
     const int i = row / s.G, h = hk * s.G + (row - i * s.G), blocks = (s.rows + 15) / 16;
     const int64_t step = 16 * (s.D + 2);
     const float* const at = a.part + (((int64_t)b * s.HKV + hk) * blocks + (row >> 4)) * a.parts * step;
     const float inf = f32_of_bits(0x7F800000u);
-    float m = -inf, l = 0.f, o = 0.f;
-    for (int n = 0; n < a.parts; ++n) m = fmaxf(m, at[n * step + rr]);
-    for (int n = 0; n < a.parts; ++n) {
-        const float mn = at[n * step + rr], ln = at[n * step + 16 + rr];
-        const float f = mn == -inf ? 1.f : __builtin_amdgcn_exp2f(mn - m);
-        l += ln * f;
-        if (d < s.D) {
-            const float v = at[n * step + 32 + rr * s.D + d];
-            o += v - v == 0.f ? v * f : v;
-        }
+    float mine[AT_MOST_PARTS / 128], sums[AT_MOST_PARTS / 128], m = -inf, l = 0.f;
+#pragma unroll
+    for (int x = 0; x < AT_MOST_PARTS / 128; ++x) {
+        const int n = t + 128 * x;
+        mine[x] = n < a.parts ? at[n * step + rr] : -inf;
+        sums[x] = n < a.parts ? at[n * step + 16 + rr] : 0.f;
+        m = fmaxf(m, mine[x]);
     }
-    if (a.lse && d == 0) a.lse[((int64_t)b * s.HKV * s.G + h) * s.LQ + i] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
-    if (d < s.D) {
-        const int64_t to = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + h) * s.D + d;
-        const float v = l == 0.f ? 0.f : o / l;
-        store_value(a.o, to, a.ko, a.fo, v);
-        if (a.copy) store_value(a.copy, to, a.kc, a.fc, v);
+    m = wave_max(m);
+    if ((t & 63) == 0) half_max[t >> 6] = m;
+    __syncthreads();
+    m = fmaxf(half_max[0], half_max[1]);
+#pragma unroll
+    for (int x = 0; x < AT_MOST_PARTS / 128; ++x) {
+        const float f = mine[x] == -inf ? 1.f : __builtin_amdgcn_exp2f(mine[x] - m);  // a part without keys: zeros, or NaN
+        weight[t + 128 * x] = f;
+        l += sums[x] * f;
     }
+    l = wave_sum(l);
+    if ((t & 63) == 0) half_sum[t >> 6] = l;
+    __syncthreads();
+    l = half_sum[0] + half_sum[1];
+    if (a.lse && t == 0) a.lse[((int64_t)b * s.HKV * s.G + h) * s.LQ + i] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
+    if (t >= s.D) return;
+    const float* const from = at + 32 + rr * s.D + t;
+    float o = 0.f;
+    for (int n = 0; n < a.parts; n += 8) {
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = from[(n + x < a.parts ? n + x : 0) * step];
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            if (n + x < a.parts) o += v[x] - v[x] == 0.f ? v[x] * weight[n + x] : v[x];
+    }
+    const int64_t to = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + h) * s.D + t;
+    o = l == 0.f ? 0.f : o / l;
+    store_value(a.o, to, a.ko, a.fo, o);
+    if (a.copy) store_value(a.copy, to, a.kc, a.fc, o);
 }
 
 }  // namespace pnn
