@@ -125,13 +125,11 @@ void launch_bwd(hipStream_t st, const Plan& p, const AttnBwd& a) {
 }
 
 template <int K>
-void launch_token(hipStream_t st, int db, bool two, const dim3& grid, const AttnToken& a) {
+void launch_token(hipStream_t st, int db, const dim3& grid, const AttnToken& a) {
     const bool whole = a.s.D % 8 == 0;
-#define PNN_TOKEN(DB)                                                                                                    \
-    if (two && whole) hipLaunchKernelGGL((attn_token_kernel<K, DB, true, true>), grid, dim3(256), 0, st, a);             \
-    else if (two) hipLaunchKernelGGL((attn_token_kernel<K, DB, true, false>), grid, dim3(256), 0, st, a);                \
-    else if (whole) hipLaunchKernelGGL((attn_token_kernel<K, DB, false, true>), grid, dim3(256), 0, st, a);              \
-    else hipLaunchKernelGGL((attn_token_kernel<K, DB, false, false>), grid, dim3(256), 0, st, a);
+#define PNN_TOKEN(DB)                                                                                   \
+    if (whole) hipLaunchKernelGGL((attn_token_kernel<K, DB, true>), grid, dim3(256), 0, st, a);         \
+    else hipLaunchKernelGGL((attn_token_kernel<K, DB, false>), grid, dim3(256), 0, st, a);
     switch (db) {
         case 1: PNN_TOKEN(1) break;
         case 2: PNN_TOKEN(2) break;
@@ -169,7 +167,6 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     discard_stale_hip_error();
     Plan p = make_plan(d);
     p.s.lens = lens;
-    const bool two = fout != PNN_BF16;  // the probabilities to 16 bits
     const TokenPlan tp = token_plan(d);
     if (tp.use) {
         AttnToken a = {};
@@ -180,9 +177,9 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
         a.tiles = tp.tiles; a.parts = tp.parts; a.part = (float*)workspace;
         const dim3 grid((unsigned)(tp.blocks * tp.parts), (unsigned)d.HKV, (unsigned)d.B);
         switch (kind_of(fkv)) {
-            case KIND_POSIT_U8: launch_token<KIND_POSIT_U8>(st, p.db, two, grid, a); break;
-            case KIND_POSIT_U16: launch_token<KIND_POSIT_U16>(st, p.db, two, grid, a); break;
-            default: launch_token<KIND_BF16>(st, p.db, two, grid, a); break;
+            case KIND_POSIT_U8: launch_token<KIND_POSIT_U8>(st, p.db, grid, a); break;
+            case KIND_POSIT_U16: launch_token<KIND_POSIT_U16>(st, p.db, grid, a); break;
+            default: launch_token<KIND_BF16>(st, p.db, grid, a); break;
         }
         if (tp.parts > 1) hipLaunchKernelGGL(attn_join_kernel, dim3((unsigned)p.s.rows, (unsigned)d.HKV, (unsigned)d.B), dim3(128), 0, st, a);
         return hip_status(hipGetLastError());
@@ -200,7 +197,8 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     a.ko = kind_of(fout); a.fo = elem_fmt(fout); a.kc = kind_of(o_copy ? fcopy : fout); a.fc = elem_fmt(o_copy ? fcopy : fout);
     a.nbh = (int)p.nbh;
     a.flags = flags; a.vsrc = v; a.vb = d.vb; a.vl = d.vl; a.vh = d.vh; a.kv = kind_of(fkv); a.fv = elem_fmt(fkv);
-    if (two) launch_fwd<true>(st, p, a);
+    // the probabilities to 16 bits where the result's format keeps more than 8
+    if (fout != PNN_BF16) launch_fwd<true>(st, p, a);
     else launch_fwd<false>(st, p, a);
     return hip_status(hipGetLastError());
 }

@@ -44,19 +44,6 @@ __device__ __forceinline__ void at_landed() {
 }
 
 // Positions, rows and blocks of one sequence fit 32 bits; offsets into tensors do not.
-// Positions, rows and blocks of one sequence fit 32 bits; offsets into tensors do not.
-// N matrix instructions with an LDS read each: AHEAD reads in front, then one read for each instruction.
-template <int N, int AHEAD>
-__device__ __forceinline__ void at_order() {
-    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
-#pragma unroll
-    for (int i = 0; i < N - AHEAD; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
-}
-
 struct AttnShape {
     int LQ, LK;
     int window, sinks;      // window 0: none, which any of LK keys or more is; sinks at most LK

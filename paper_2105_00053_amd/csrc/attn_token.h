@@ -65,7 +65,7 @@ __device__ __forceinline__ void at_words(const T* src, int left, uint32_t (&o)[N
 
 // WHOLE: heads of a multiple of 8 elements, so that a vector lies inside one or outside; those outside are read from the head's start and, of keys,
 // taken as zero (of values they go to elements that do not exist).
-template <int K, int DB, bool TWO, bool WHOLE>
+template <int K, int DB, bool WHOLE>
 __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void attn_token_kernel(AttnToken a) {
     constexpr int KS = DB, NV = DB <= 2 ? 4 : 8;
     __shared__ uint32_t smem[8192];  // the table, then what the waves join through
@@ -227,14 +227,14 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             ph[r] = (__bf16)sc[r];
-            if (TWO) pl[r] = (__bf16)(sc[r] - (float)ph[r]);
+            pl[r] = (__bf16)(sc[r] - (float)ph[r]);
         }
 #pragma unroll
         for (int x = 0; x < NV; ++x) {
             const at_v8b v = at_frag(make_uint4(pair(cur.v[0], x, cur.v[1], x, true), pair(cur.v[2], x, cur.v[3], x, true), pair(cur.v[4], x, cur.v[5], x, true),
                                                 pair(cur.v[6], x, cur.v[7], x, true)));
             o[x] = at_mfma16(v, ph, o[x]);
-            if (TWO) o[x] = at_mfma16(v, pl, o[x]);
+            o[x] = at_mfma16(v, pl, o[x]);
         }
     }
     l += __shfl_xor(l, 16, 64);
