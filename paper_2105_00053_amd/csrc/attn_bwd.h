@@ -156,14 +156,16 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
 
 // 64 keys to a workgroup, NP blocks of 32 rows at a time: of its 2 NP waves, NP take each block of 32 keys, each with every NP-th block of
 // rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few, so the length of the longest
-// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four see below.
+// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four 139.
 constexpr int at_parallel(int db) { return db <= 2 ? 4 : 2; }  // what LDS (128 KB) holds of two stages
 
 template <int DB, bool TWO>
 __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_dkv_kernel(AttnBwd a) {
     constexpr int KS = 2 * DB, NP = at_parallel(DB), RUNS = 4 * KS;  // 1 KB runs of a block of rows: q, d_o, both transposed
-    __shared__ uint4 buf[2][NP][RUNS * 64];
-    __shared__ __attribute__((aligned(16))) float stats[2][NP][AT_STATS];
+    // One object for the operands and the rows' statistics behind them: between two, the compiler waits for all copies in front of the first read of
+    // either, those for the next round among them.
+    constexpr int ROUND = RUNS * 64 + AT_STATS / 4;
+    __shared__ uint4 buf[2][NP][ROUND];
     const AttnShape& s = a.s;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, turn = w >> 1;
     const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh;
@@ -198,7 +200,7 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
 #pragma unroll
             for (int r = 0; r < KS; ++r) at_copy(src[x] + at + r * 64, dst + r * 64, lane);
         }
-        if ((w & 1) == 0 && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + blk) * AT_STATS), (uint4*)stats[n & 1][turn], lane);
+        if ((w & 1) == 0 && lane < AT_STATS / 4) at_copy((const uint4*)(a.stats + (rows0 + blk) * AT_STATS), buf[n & 1][turn] + RUNS * 64, lane);
     };
 
     at_v16f dk[DB], dv[DB];
@@ -217,7 +219,7 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
         if (n + 1 < rounds) issue(n + 1);
         if (NP * n + turn >= blocks) continue;
         const uint4* rb = buf[n & 1][turn] + lane;
-        const float* st = stats[n & 1][turn];
+        const float* st = (const float*)(buf[n & 1][turn] + RUNS * 64) + 4 * half;
         const int row0 = (last - NP * n - turn) * 32, p0 = base + quot, p1 = p0 + reach;  // p1: the last row's position or more
         quot -= NP * 32 / s.G;
         rem -= NP * 32 % s.G;
@@ -235,18 +237,18 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
             dp = at_mfma(at_frag(rb[(KS + ks) * 64]), vf[ks], dp);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -st[at_row(r, half)]));
+        for (int r = 0; r < 16; ++r) {
+            sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -st[at_row(r, 0)]));
+            dp[r] -= st[32 + at_row(r, 0)];
+        }
         if (!whole) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int p = __builtin_bit_cast(int, st[64 + at_row(r, half)]);
+                const int p = __builtin_bit_cast(int, st[64 + at_row(r, 0)]);
                 const bool see = at_sees(s, p, s.window ? p - s.window : -1, key);
                 sc[r] = see ? sc[r] : 0.f;
-                dp[r] = see ? dp[r] - st[32 + at_row(r, half)] : 0.f;
+                dp[r] = see ? dp[r] : 0.f;
             }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] -= st[32 + at_row(r, half)];
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[r] *= sc[r];

@@ -59,7 +59,7 @@ __device__ __forceinline__ int at_keys(const AttnShape& s, int64_t b) {
     return n < 0 ? 0 : (n > s.LK ? s.LK : n);
 }
 // whether a query at position p sees a key; low = the last position in front of its window
-__device__ __forceinline__ bool at_sees(const AttnShape& s, int p, int low, int key) { return key <= p && (key > low || key < s.sinks); }
+__device__ __forceinline__ bool at_sees(const AttnShape& s, int p, int low, int key) { return (key <= p) & ((key > low) | (key < s.sinks)); }
 
 // Order of n tiles whose work falls with their number, for nbh heads each: back and forth over as many tiles as fill the chip's 256 compute
 // units once, so that the workgroups that share a unit have about the same work together.
