@@ -90,15 +90,15 @@ __device__ __forceinline__ void lp_bound(LogprobTop& sh, lp_key best, uint32_t s
     best = lp_sort(best);
     sh.sorted[w][lane] = best;
     __syncthreads();
-    int rank = lane;
-    for (int o = 1; o < 4; ++o) {
-        const lp_key* s = sh.sorted[(w + o) & 3];
-        int at = 0;  // keys of the other wave that are larger
+    int at[3] = {0, 0, 0};  // keys of the other waves that are larger; all reads are issued, so that the three searches' latencies overlap
 #pragma unroll
-        for (int step = 64; step >= 1; step /= 2)
-            if (at + step <= 64 && s[at + step - 1] > best) at += step;
-        rank += at;
-    }
+    for (int step = 64; step >= 1; step /= 2)
+#pragma unroll
+        for (int o = 0; o < 3; ++o) {
+            const int to = at[o] + step, x = to <= 64 ? to - 1 : 63;
+            at[o] = (sh.sorted[(w + o + 1) & 3][x] > best) & (to <= 64) ? to : at[o];
+        }
+    const int rank = lane + at[0] + at[1] + at[2];
     if (rank == k - 1 && best != 0) sh.bound = best - slack;
 }
 
@@ -119,7 +119,9 @@ __device__ __forceinline__ void lp_select(LogprobTop& sh, int k, Visit visit) {
         for (int i = t; i < count; i += 256) {
             const lp_key key = sh.list[i];
             int r = 0;
-            for (int j = 0; j < count && r < k; ++j) r += sh.list[j] > key ? 1 : 0;
+            for (int j = 0; j < count && r < k; j += 8)  // eight reads in flight; the list's length is a multiple of 8
+#pragma unroll
+                for (int x = 0; x < 8; ++x) r += (sh.list[j + x] > key) & (j + x < count) ? 1 : 0;
             if (r < k) sh.result[r] = key;
         }
     } else {
@@ -152,19 +154,23 @@ __device__ __forceinline__ void lp_clear(LogprobTop& sh) {
     }
 }
 
-__device__ __forceinline__ float lp_block_sum(float v, float* part) {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
-}
+// A workgroup's maximum, and two of its sums; each once in a kernel, in words of `part` (12) of its own.
 __device__ __forceinline__ float lp_block_max(float v, float* part) {
     v = wave_max(v);
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     return fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+__device__ __forceinline__ void lp_block_sums(float& s, float& u, float* part) {
+    s = wave_sum(s);
+    u = wave_sum(u);
+    if ((threadIdx.x & 63) == 0) {
+        part[4 + (threadIdx.x >> 6)] = s;
+        part[8 + (threadIdx.x >> 6)] = u;
+    }
+    __syncthreads();
+    s = (part[4] + part[5]) + (part[6] + part[7]);
+    u = (part[8] + part[9]) + (part[10] + part[11]);
 }
 
 // A row's outputs from its maximum m (of z'), sums and alternatives; by all threads.
@@ -196,7 +202,7 @@ template <int K>
 __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     constexpr int B = sizeof(typename Raw<K>::T), W = 2 * B, NC = 64 / W;  // words of a vector of 8, vectors to a thread
     constexpr bool POSIT = K == KIND_POSIT_U8 || K == KIND_POSIT_U16;
-    __shared__ float part[4];
+    __shared__ float part[12];
     __shared__ LogprobTop sh;
     __shared__ uint32_t hist[K == KIND_POSIT_U8 ? 256 * LP_COPIES : 1];
     const int t = threadIdx.x;
@@ -302,8 +308,9 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
         bad = __syncthreads_or(nar && count > 0);
         m = lp_block_max(count > 0 && !nar ? v : -inf, part);
         const float d = v - m, e = count > 0 ? (float)count * __builtin_amdgcn_exp2f(d * LP_LOG2E) : 0.f;
-        s = lp_block_sum(e, part);
-        u = lp_block_sum(e > 0.f ? e * d : 0.f, part);
+        s = e;
+        u = e > 0.f ? e * d : 0.f;
+        lp_block_sums(s, u, part);
         if (a.top > 0) {
             // logits in the bins from the largest value down to thread t's, 127 - t for what is not negative: where they reach k is the bound
             uint32_t* const down = hist;
@@ -343,8 +350,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
                 s += x;
                 u = fmaf(x, POSIT ? d : fmaxf(d, -200.f), u);
             }
-            s = lp_block_sum(s, part);
-            u = lp_block_sum(u, part);
+            lp_block_sums(s, u, part);
             bad = bad || !(s == s) || m == inf;
         } else if (!POSIT) {
             // nothing but -inf, and NaN perhaps
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
 
 // Parts of a row joined, one row to a workgroup.
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobFwd a) {
-    __shared__ float part[4];
+    __shared__ float part[12];
     __shared__ LogprobTop sh;
     const int64_t row = blockIdx.x;
     const int t = threadIdx.x;
@@ -433,8 +439,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobFwd a) {
         s = fmaf(f, x.y, s);
         if (f > 0.f) u = fmaf(f, fmaf(x.y, d, x.z), u);
     }
-    s = lp_block_sum(s, part);
-    u = lp_block_sum(u, part);
+    lp_block_sums(s, u, part);
     if (a.top > 0) {
         const lp_key* const keys = a.part_keys + row * a.parts * a.top;
         const int64_t n = (int64_t)a.parts * a.top;
@@ -504,6 +509,9 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwd a) {
 // Logits of a part: what 256 threads hold in 64 words each, less where that leaves most of the chip without work.
 inline int64_t logprob_span(int fz, int64_t rows, int64_t vocab) {
     int64_t span = 16 * 2048 * 2 / (int64_t)element_bytes(fz);
+    // A row that fits one workgroup's registers stays whole: the second kernel costs more than the parts save (32 rows, five alternatives, us: 5003 logits in
+    // binary32 8.0 and 11.9, 16384 in 16-bit posits 10.9 and 12.8, 50021 in 8-bit ones 14.0 and 14.6; 32000 in 16-bit ones 14.4 and 13.5).
+    if (vocab <= span) return span;
     while (span > 2048 && rows * ((vocab + span - 1) / span) < 512) span /= 2;
     return span;
 }

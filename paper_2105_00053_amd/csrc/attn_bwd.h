@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
 
 // 64 keys to a workgroup, NP blocks of 32 rows at a time: of its 2 NP waves, NP take each block of 32 keys, each with every NP-th block of
 // rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few, so the length of the longest
-// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four 139.
+// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four 115 to 125.
 constexpr int at_parallel(int db) { return db <= 2 ? 4 : 2; }  // what LDS (128 KB) holds of two stages
 
 template <int DB, bool TWO>
