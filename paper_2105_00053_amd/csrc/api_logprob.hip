@@ -8,6 +8,9 @@
 // Alternatives.  Each thread's largest logit (with the place of its vector) is sorted among the 256: the k-th largest of these
 // bounds the k-th largest of all from below, and few logits are above it (about k + k^2 / 512 for random ones).  Those are collected and ranked by
 // counting.  Where more are above it than the list holds, k rounds of a maximum take its place.
+// What bounds it: the launch where rows are few (one of 100003 16-bit posits, 20 alternatives: 9 us and 7 for the join of 49 parts), an atomic addition in
+// LDS a logit of 8 bits (2048 rows of 50021, 8 alternatives: 42 us for 102 MB, 2.5 TB/s), the vector unit's decoding and exponentials for 16 bits (4096 rows of 32000:
+// 97 to 104 us for 262 MB, 2.6 TB/s).
 #include "lm_codec.h"
 
 namespace pnn {
@@ -469,7 +472,8 @@ struct LogprobBwd {
     int parts;
 };
 
-// Bound by memory: a part of a row to a workgroup, vectors of 8 to a thread, the next one in flight.
+// Bound by memory: a part of a row to a workgroup, vectors of 8 to a thread, the next one in flight.  4096 rows of 32000 16-bit posits to
+// bfloat16: 117 to 130 us for 524 MB, 4.3 TB/s.
 template <int K>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwd a) {
     const int t = threadIdx.x;

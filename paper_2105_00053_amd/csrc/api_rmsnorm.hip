@@ -1,4 +1,8 @@
 // posit_rmsnorm_fwd / posit_rmsnorm_bwd / posit_scale_rows: the RMS norm of a residual stream, its gradient, and rows times scales.
+//
+// y = h w / sqrt(mean h^2 + eps), h = x + r.  Bound by memory where rows are many, by the launch where they are few.  16384 rows of 4096, 8-bit
+// posits on a stream of 16-bit ones to bfloat16: forward 122 to 145 us for 470 MB (3.9 TB/s; a large copy reaches 5.2), backward 112 to 117 for
+// 537 MB.  4099 rows of 5119, odd pitches, bfloat16 stream to 8-bit posits with scales: 56 to 60; four rows of 2048: 5.
 #include "lm_codec.h"
 
 namespace pnn {
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_kernel(NormBwd a) {
     store_value(a.dw, j, a.kdw, a.fdw, s);
 }
 
-// 8 elements to a thread
+// 8 elements to a thread; 4099 x 5119 in 8-bit posits 21 us (both sides unaligned), four rows of 2048 2.
 __global__ __launch_bounds__(256) void scale_rows_kernel(const void* x, int64_t ldx, int kx, ElemFmt fx, const float* scale, void* y, int64_t ldy, int ky, ElemFmt fy,
                                                          int64_t rows, int64_t cols, uint32_t vectors) {
     const uint32_t id = blockIdx.x * 256u + threadIdx.x, r = id / vectors;

@@ -1,10 +1,12 @@
 // Gradients of attention, from recomputed probabilities: P = exp(S - lse), dS = P * (dP - D) with dP = dO V^T and D = rowsum(dO * o).
 //
 // Two kernels, so that every sum has one owner and a fixed order (no atomics): one walks the keys of 128 rows (dQ), as the forward kernel
-// does; one walks the rows that see 128 keys (dK and dV), where the heads that share a key are rows like others.  In both
+// does; one walks the rows that see 64 keys (dK and dV), where the heads that share a key are rows like others.  In both
 // the products that reduce over a head's elements come out in the lane order that the next product wants its operand in.
 //   rows:  S^T = K Q^T and dP^T = V dO^T (a lane holds one row: lse and D are its own), dQ^T += K^T dS^T
 //   keys:  S = Q K^T and dP = dO V^T (a lane holds one key), dV^T += dO^T P, dK^T += Q^T dS
+// As the forward kernel, bound by LDS reads and the vector unit beside the matrix unit.  4 sequences of 2048, 16 heads on 4 of 64, causal, bfloat16 out:
+// rows 63 to 66 us, keys 115 to 122 (0.8 and 0.6 PFLOP/s), rows' statistics 12.
 #pragma once
 
 #include "attn_prompt.h"
@@ -156,7 +158,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnBwd a) {
 
 // 64 keys to a workgroup, NP blocks of 32 rows at a time: of its 2 NP waves, NP take each block of 32 keys, each with every NP-th block of
 // rows, and join their sums at the end.  With a causal mask the first keys are seen by all rows and the last by few, so the length of the longest
-// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four 115 to 125.
+// workgroup decides: 4 sequences of 2048, 64 elements a head, us: 128 keys and one block of rows at a time 250, 64 keys and two 164, four 115 to 122.  Both
+// blocks of keys in one wave, with rows' operands straight from memory into registers, take LDS and the barriers away and come to 128: with one wave to a SIMD
+// results move between the two register files.
 constexpr int at_parallel(int db) { return db <= 2 ? 4 : 2; }  // what LDS (128 KB) holds of two stages
 
 template <int DB, bool TWO>
