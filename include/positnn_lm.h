@@ -64,7 +64,7 @@ int posit_scale_rows(void* stream, int fin, int fout, int64_t rows, int64_t cols
  * A query that sees nothing (p < 0) has o = 0 and lse = -inf.  Only what a query sees can make its output NaN.
  * Formats: q in fq, k and v in fkv, one of those that bfloat16 holds exactly: posit<8,0>, (8,1), (8,2), (10,1), (10,2),
  * (12,2) and PNN_BF16 (else PNN_EUNSUPPORTED); o in any element format.  Products of q and k are exact; the
- * probabilities go into the second product rounded to 16 bits, or to 8 where o is PNN_BF16, which keeps no more.
+ * probabilities go into the second product rounded to 16 bits, or to 8 where o and o_copy are PNN_BF16, which keeps no more.
  * Strides are in elements; the elements of a head are contiguous.  Output layouts: o dense [b][i][h][d]. */
 typedef struct {
     int64_t B, HQ, HKV, LQ, LK, D;   /* D <= 128, HQ a multiple of HKV */

@@ -372,15 +372,19 @@ struct NormPlan {
     int T, threads;
     unsigned groups;
 };
-inline NormPlan norm_plan(int64_t rows, int64_t cols) {
+inline NormPlan norm_plan(int64_t rows, int64_t cols, int waves) {
     NormPlan p = {cols <= 8192, 1024, 1024, 0};
     if (p.rows) p.T = (int)((cols + 511) / 512) * 64;
     p.threads = p.T == 64 || p.T == 128 ? 256 : p.T;
-    // as many workgroups as the chip holds, 2048 threads to a compute unit; each walks over rows
-    const int64_t want = (rows + p.threads / p.T - 1) / (p.threads / p.T), most = 256 * (2048 / p.threads);
+    // as many workgroups as the chip holds, each walking over rows; `waves` of them to a compute unit, by the kernels' registers
+    const int64_t want = (rows + p.threads / p.T - 1) / (p.threads / p.T), most = 256 * (waves * 64 / p.threads);
     p.groups = (unsigned)(want < most ? want : most);
     return p;
 }
+
+// What the kernels' registers leave room for (forward up to 72 of 512, backward up to 128).  us with 32, 28 and 16 waves to a compute unit: forward, 4099 rows of
+// 5119, 51, 45 and 66; 16384 of 4096, 101, 97 and 107; backward 75, 70 and 64; 94, 92 and 87; 2000 rows of 3000, 31, 27 and 22.
+constexpr int NORM_FWD_WAVES = 28, NORM_BWD_WAVES = 16;
 
 template <int KX>
 void launch_fwd_rows(hipStream_t st, const NormPlan& p, const NormFwd& a) {
@@ -421,7 +425,7 @@ extern "C" int posit_rmsnorm_fwd(void* stream, int fx, int fres, int fw, int fy,
     NormFwd a = {x, res, w, res_out, y, scale, rstd, rows, cols, ldx, ldr, ldo, ldy, eps, kind_of(fx), res ? kind_of(fres) : 0, kind_of(fw), kind_of(fy),
                  elem_fmt(fx), elem_fmt(res ? fres : fx), elem_fmt(fw), elem_fmt(fy)};
     hipStream_t st = (hipStream_t)stream;
-    const NormPlan p = norm_plan(rows, cols);
+    const NormPlan p = norm_plan(rows, cols, NORM_FWD_WAVES);
     if (p.rows) {
         PNN_DISPATCH_KIND(a.kx, launch_fwd_rows<K>(st, p, a))
     } else hipLaunchKernelGGL(rmsnorm_fwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
@@ -430,7 +434,7 @@ extern "C" int posit_rmsnorm_fwd(void* stream, int fx, int fres, int fw, int fy,
 
 extern "C" size_t posit_rmsnorm_bwd_workspace(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0 || cols > 8192) return 0;
-    return (size_t)norm_plan(rows, cols).groups * (size_t)cols * 4;
+    return (size_t)norm_plan(rows, cols, NORM_BWD_WAVES).groups * (size_t)cols * 4;
 }
 
 extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres, int fdx, int fdw, int64_t rows, int64_t cols, const void* dy, int64_t lddy,
@@ -449,7 +453,7 @@ extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres
     NormBwd a = {dy, h, w, dres, rstd, dx, dw, rows, cols, lddy, ldh, lddr, lddx, kind_of(fd), kind_of(fh), kind_of(fw), kind_of(dres ? fdres : fd), kind_of(fdx),
                  kind_of(dw ? fdw : fd), elem_fmt(fd), elem_fmt(fh), elem_fmt(fw), elem_fmt(dres ? fdres : fd), elem_fmt(fdx), elem_fmt(dw ? fdw : fd), (float*)workspace};
     hipStream_t st = (hipStream_t)stream;
-    const NormPlan p = norm_plan(rows, cols);
+    const NormPlan p = norm_plan(rows, cols, NORM_BWD_WAVES);
     if (p.rows) {
         PNN_DISPATCH_KIND(a.kd, launch_bwd_rows_of<K>(st, p, a))
         if (dw) hipLaunchKernelGGL(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, st, a.part, (int)p.groups, cols, dw, a.kdw, a.fdw);
