@@ -84,6 +84,21 @@ Plan make_plan(const pnn_attention_desc& d) {
     return p;
 }
 
+// Workgroups to a tile of 64 keys in the backward pass: one holds a compute unit's LDS, so where tiles are fewer than half the chip's units their rows are
+// shared out, at least two rounds of blocks to a workgroup (forward and backward pass of 2 sequences of 976, 4 heads on one of 40, window 53: 95 us, now 58;
+// of 840, 4 on one of 64, causal: 97 and 76).
+int dkv_parts(const Plan& p) {
+    const int64_t tiles = p.nbh * (p.s.kblocks / 2), rounds = p.s.qblocks / at_parallel(p.db);
+    if (tiles == 0) return 1;
+    int64_t parts = 256 / tiles;
+    if (parts > rounds / 2) parts = rounds / 2;
+    return parts > 1 ? (int)parts : 1;
+}
+int64_t dkv_part_bytes(const Plan& p) {
+    const int parts = dkv_parts(p);
+    return parts > 1 ? parts * p.nbh * p.s.LK * 2 * p.s.D * 4 : 0;
+}
+
 void launch_pack(hipStream_t st, const Plan& p, const AttnPack& a, int items) {
     int64_t blocks = 0;
     for (int i = 0; i < items; ++i) blocks = a.item[i].blocks > blocks ? a.item[i].blocks : blocks;
@@ -111,7 +126,9 @@ void launch_fwd(hipStream_t st, const Plan& p, const AttnFwd& a) {
 template <int DB, bool TWO>
 void launch_bwd_of(hipStream_t st, const Plan& p, const AttnBwd& a) {
     if (p.s.LQ > 0) hipLaunchKernelGGL((attn_dq_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.qblocks / 4))), dim3(256), 0, st, a);
-    if (p.s.LK > 0) hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 2))), dim3(128 * at_parallel(DB)), 0, st, a);
+    if (p.s.LK == 0) return;
+    hipLaunchKernelGGL((attn_dkv_kernel<DB, TWO>), dim3((unsigned)(p.nbh * (p.s.kblocks / 2) * a.parts)), dim3(128 * at_parallel(DB)), 0, st, a);
+    if (a.parts > 1) hipLaunchKernelGGL(attn_dkv_join_kernel, dim3((unsigned)((p.nbh * p.s.LK * 2 * p.s.D + 255) / 256)), dim3(256), 0, st, a);
 }
 
 template <bool TWO>
@@ -147,7 +164,7 @@ extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attent
     const TokenPlan t = token_plan(*desc);
     if (which == 0 && t.use) return (size_t)t.bytes;
     if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
-    return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4));
+    return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4) + dkv_part_bytes(p));
 }
 
 extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, const pnn_attention_desc* desc, const void* q, const void* k, const void* v,
@@ -243,6 +260,7 @@ extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo
     AttnBwd a = {};
     a.s = p.s; a.q = wq; a.g = wg; a.qt = wqt; a.gt = wgt; a.k = wk; a.v = wv; a.kt = wkt; a.stats = stats; a.dq = dq; a.dk = dk; a.dv = dv;
     a.kout = kind_of(fout); a.fout = elem_fmt(fout); a.nbh = (int)p.nbh;
+    a.parts = dkv_parts(p); a.part = (float*)(flags + p.nbh * p.s.qblocks);
     a.flags = flags; a.gsrc = d_o; a.gb = d.qb; a.gl = d.ql; a.gh = d.qh; a.kg = kind_of(fd); a.fg = elem_fmt(fd);
     if (fout == PNN_BF16) launch_bwd<false>(st, p, a);
     else launch_bwd<true>(st, p, a);

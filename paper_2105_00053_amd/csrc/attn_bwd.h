@@ -30,6 +30,8 @@ struct AttnBwd {
     int64_t gb, gl, gh;
     int kg;
     ElemFmt fg;
+    int parts;                    // workgroups to a tile of keys; each of them leaves its rows' sums in `part`, [part][batch, head][key][dK, dV][element]
+    float* part;
 };
 
 struct AttnStats {
@@ -172,7 +174,7 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
     __shared__ uint4 buf[2][NP][ROUND];
     const AttnShape& s = a.s;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), half = lane >> 5, turn = w >> 1;
-    const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh;
+    const int bh = blockIdx.x % (unsigned)a.nbh, tile = blockIdx.x / (unsigned)a.nbh / (unsigned)a.parts, share = blockIdx.x / (unsigned)a.nbh - tile * a.parts;
     const int b = bh / s.HKV, hk = bh - b * s.HKV, keys = at_keys(s, b), base = keys - s.LQ;
     const int k0 = tile * 64, kw = k0 + (w & 1) * 32, key = kw + (lane & 31);
     const float c = s.scale * 1.4426950408889634f;
@@ -180,7 +182,13 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
     const int i0 = k0 - base > 0 ? k0 - base : 0;
     int64_t i1 = s.LQ - 1;
     if (s.window && k0 >= s.sinks && (int64_t)k0 + 62 + s.window - base < i1) i1 = (int64_t)k0 + 62 + s.window - base;
-    const int first = (int)((int64_t)i0 * s.G / 32), blocks = k0 >= keys || i0 > i1 ? 0 : (int)((i1 * s.G + s.G - 1) / 32) - first + 1;
+    int first = (int)((int64_t)i0 * s.G / 32), blocks = k0 >= keys || i0 > i1 ? 0 : (int)((i1 * s.G + s.G - 1) / 32) - first + 1;
+    if (a.parts > 1) {  // whole rounds, the first share at the end of the rows
+        const int chunk = ((blocks + a.parts - 1) / a.parts + NP - 1) / NP * NP, rest = blocks - share * chunk;
+        const int mine = rest < 0 ? 0 : (rest < chunk ? rest : chunk);
+        first += rest - mine;
+        blocks = mine;
+    }
 
     at_v8b kf[KS], vf[KS];
     const int64_t mine = (int64_t)bh * s.kblocks + tile * 2 + (w & 1);
@@ -320,8 +328,9 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
                     }
             }
         }
-    const int64_t at = (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
-    void* const out = turn ? a.dv : a.dk;
+    const int64_t at = a.parts > 1 ? (((share * (int64_t)a.nbh + bh) * s.LK + key) * 2 + turn) * s.D : (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
+    void* const out = a.parts > 1 ? a.part : (turn ? a.dv : a.dk);
+    const int kind = a.parts > 1 ? KIND_F32 : a.kout;
     const float up = turn ? 1.f : s.scale;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
@@ -330,8 +339,19 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
             dk[d][r] *= up;
             if (flagged) dk[d][r] = marks.apply(16 * d + r, dk[d][r]);
         }
-        at_eights(dk[d], half, [&](int e, const float (&v)[8]) { at_store8(out, at + d * 32 + e, s.D - d * 32 - e, a.kout, a.fout, v); });
+        at_eights(dk[d], half, [&](int e, const float (&v)[8]) { at_store8(out, at + d * 32 + e, s.D - d * 32 - e, kind, a.fout, v); });
     }
+}
+
+// The shares of a tile's rows added up, an element of dK or dV to a thread.
+__global__ __launch_bounds__(256) void attn_dkv_join_kernel(AttnBwd a) {
+    const AttnShape& s = a.s;
+    const int64_t n = (int64_t)a.nbh * s.LK * 2 * s.D, x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (x >= n) return;
+    float v = 0.f;
+    for (int y = 0; y < a.parts; ++y) v += a.part[y * n + x];
+    const int64_t row = x / s.D, key = (row >> 1) % s.LK, bh = (row >> 1) / s.LK, b = bh / s.HKV, hk = bh - b * s.HKV;
+    store_value((row & 1) ? a.dv : a.dk, ((b * s.LK + key) * s.HKV + hk) * s.D + (x - row * s.D), a.kout, a.fout, v);
 }
 
 }  // namespace pnn

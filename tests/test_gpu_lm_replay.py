@@ -60,3 +60,28 @@ def test_graph_replays():
         for n, (a, c) in enumerate(zip(got, want)):
             a, c = (t.view(torch.int16) if t.dtype == torch.uint16 else t for t in (a, c))
             assert torch.equal(a, c), (seed, n)
+
+
+@pytest.mark.parametrize("b,l,hq,hkv,d", [(1, 331, 5, 1, 40), (2, 520, 2, 1, 64), (1, 300, 8, 1, 128), (1, 700, 6, 2, 96)])
+def test_gradients_of_few_heads_over_many_rows(b, l, hq, hkv, d):
+    """Tiles of keys whose rows are shared out over workgroups."""
+    _, q, k, v, do = _inputs(b, l, l, hq, hkv, d, "p8_2", "p8_2", 33)
+    _compare(q, k, v, do, "p8_2", "p8_2", "bf16")
+    _compare(q, k, v, do, "p8_2", "p8_2", "f32", window=53, sinks=4, lens=[l - 97 * (i + 1) for i in range(b)])
+
+
+def test_nar_in_a_row_of_a_shared_tile():
+    """A NaR in one row of the output's gradient: dV of the keys that the row sees is NaN, of the others what it is without."""
+    l, d = 400, 32
+    _, q, k, v, do = _inputs(1, l, l, 4, 1, d, "p8_2", "p8_2", 34)
+    o, lse, copy = pn.posit_attention_fwd(q, k, v, "p8_2", "p8_2", "bf16", fcopy="f32", window=60)
+    back = lambda g: pn.posit_attention_bwd(g, q, k, v, copy, lse, "p8_2", "p8_2", "p8_2", "f32", "f32", window=60)  # noqa: E731
+    clean = back(do)
+    bad = do.clone()
+    bad[0, 200, 1, 7] = 128
+    got = back(bad)
+    sees = torch.zeros(l, dtype=torch.bool, device="cuda")
+    sees[141:201] = True
+    assert torch.isnan(got[2][0, sees, 0, 7]).all()
+    assert torch.equal(got[2][0, ~sees], clean[2][0, ~sees]) and torch.equal(got[1][0, ~sees], clean[1][0, ~sees])
+    assert torch.isnan(got[1][0, sees]).all()
