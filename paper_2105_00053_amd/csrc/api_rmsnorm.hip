@@ -1,8 +1,8 @@
 // posit_rmsnorm_fwd / posit_rmsnorm_bwd / posit_scale_rows: the RMS norm of a residual stream, its gradient, and rows times scales.
 //
 // y = h w / sqrt(mean h^2 + eps), h = x + r.  Bound by memory where rows are many, by the launch where they are few.  16384 rows of 4096, 8-bit
-// posits on a stream of 16-bit ones to bfloat16: forward 122 to 145 us for 470 MB (3.9 TB/s; a large copy reaches 5.2), backward 112 to 117 for
-// 537 MB.  4099 rows of 5119, odd pitches, bfloat16 stream to 8-bit posits with scales: 56 to 60; four rows of 2048: 5.
+// posits on a stream of 16-bit ones to bfloat16: forward 122 to 141 us for 470 MB (3.8 TB/s; a large copy reaches 5.2), backward 110 to 114 for
+// 537 MB.  4099 rows of 5119, odd pitches, bfloat16 stream to 8-bit posits with scales: 51; four rows of 2048: 5.
 #include "lm_codec.h"
 
 namespace pnn {

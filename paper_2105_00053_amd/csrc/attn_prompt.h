@@ -6,7 +6,8 @@
 // are.  Tiles of keys and values come through LDS, two buffers, copied straight from memory while the tile before is worked on.
 // What bounds it: a wave's 32 rows take an operand of 1 KB from LDS for each matrix instruction, which at the full matrix rate is all that LDS gives, and
 // the softmax takes the vector unit about as long as the products take the matrix unit.  2 sequences of 4001, 16 heads on 4 of 128, window 1024, to 8-bit
-// posits (probabilities in two parts): 127 to 132 us, 0.69 PFLOP/s of matrix instructions; 4 of 2048, heads of 64, causal, to bfloat16: 54, 0.64.
+// posits (probabilities in two parts): 127 to 132 us, 0.69 PFLOP/s of matrix instructions; 4 of 2048, heads of 64, causal, to bfloat16: 54, 0.64;
+// with a copy in binary32, so in two parts, 68.
 // The running maximum is a reference: results are rescaled only when a row's maximum rises by more than 2^8 above it.
 #pragma once
 
