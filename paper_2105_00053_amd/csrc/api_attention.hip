@@ -46,15 +46,16 @@ struct TokenPlan {
     int64_t bytes;
 };
 
-TokenPlan token_plan(const pnn_attention_desc& d) {
+// From make_plan's sizes: window and sinks there are at most the keys, so that their sum is small.
+TokenPlan token_plan(const AttnShape& s, int64_t B) {
     TokenPlan t = {};
-    const int64_t g = d.HKV ? d.HQ / d.HKV : 1, rows = d.LQ * g;
-    t.use = rows <= 16 || (rows <= 64 && d.LK >= 8 * rows);
+    const int64_t rows = s.rows;
+    t.use = rows <= 16 || (rows <= 64 && s.LK >= 8 * rows);
     if (!t.use) return t;
     t.blocks = (int)((rows + 15) / 16);
-    int64_t keys = d.LK;
-    if (d.window > 0 && d.window + d.LQ + d.sinks + 64 < keys) keys = d.window + d.LQ + d.sinks + 64;
-    const int64_t all = (keys + 31) / 32 + 1, groups = d.B * d.HKV * t.blocks;
+    int64_t keys = s.LK;
+    if (s.window > 0 && (int64_t)s.window + s.LQ + s.sinks + 64 < keys) keys = (int64_t)s.window + s.LQ + s.sinks + 64;
+    const int64_t all = (keys + 31) / 32 + 1, groups = B * s.HKV * t.blocks;
     // Two workgroups to a compute unit, at least a tile to each of their waves; short caches stay whole, the second kernel costs more.  48 sequences of
     // 4096 keys, 8 heads of 128: 112 us in 2 parts, 110 in 3, 124 in 4; 8 sequences of 8192: 47 in 8 parts, 52 in 16, 59 in 24.
     int64_t parts = groups > 0 ? (512 + groups - 1) / groups : 1;
@@ -64,7 +65,7 @@ TokenPlan token_plan(const pnn_attention_desc& d) {
     t.tiles = (int)((all + parts - 1) / parts);
     t.tiles = (t.tiles + 3) / 4 * 4;
     t.parts = (int)((all + t.tiles - 1) / t.tiles);
-    t.bytes = t.parts > 1 ? groups * t.parts * 16 * (d.D + 2) * 4 : 0;
+    t.bytes = t.parts > 1 ? groups * t.parts * 16 * (s.D + 2) * 4 : 0;
     return t;
 }
 
@@ -161,7 +162,7 @@ void launch_token(hipStream_t st, int db, const dim3& grid, const AttnToken& a) 
 extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attention_desc* desc) {
     if (desc_status(desc) || desc->B == 0 || desc->HQ == 0 || desc->D == 0) return 0;
     const Plan p = make_plan(*desc);
-    const TokenPlan t = token_plan(*desc);
+    const TokenPlan t = token_plan(p.s, desc->B);
     if (which == 0 && t.use) return (size_t)t.bytes;
     if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
     return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4) + dkv_part_bytes(p));
@@ -184,7 +185,7 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     discard_stale_hip_error();
     Plan p = make_plan(d);
     p.s.lens = lens;
-    const TokenPlan tp = token_plan(d);
+    const TokenPlan tp = token_plan(p.s, d.B);
     if (tp.use) {
         AttnToken a = {};
         a.s = p.s; a.q = q; a.k = k; a.v = v;
