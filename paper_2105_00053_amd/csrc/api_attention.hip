@@ -164,8 +164,8 @@ extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attent
     const Plan p = make_plan(*desc);
     const TokenPlan t = token_plan(p.s, desc->B);
     if (which == 0 && t.use) return (size_t)t.bytes;
-    if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * 4);
-    return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + 4) + dkv_part_bytes(p));
+    if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * (AT_MARKS * 16 + 4));
+    return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + AT_MARKS * 16 + 4) + dkv_part_bytes(p));
 }
 
 extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, const pnn_attention_desc* desc, const void* q, const void* k, const void* v,
@@ -204,17 +204,18 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     }
     uint4* const wk = (uint4*)workspace;
     uint4* const wv = wk + p.k_bytes / 16;
-    int32_t* const flags = (int32_t*)(wv + p.k_bytes / 16);
+    uint4* const marks = wv + p.k_bytes / 16;
+    int32_t* const flags = (int32_t*)(marks + p.nbh * p.s.kblocks * AT_MARKS);
     AttnPack pack = {};
     pack.B = (int)d.B; pack.HKV = (int)d.HKV; pack.D = (int)d.D;
-    pack.item[0] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr};
-    pack.item[1] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, nullptr, wv, 1, kind_of(fkv), elem_fmt(fkv), flags};
+    pack.item[0] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr, nullptr};
+    pack.item[1] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, nullptr, wv, 1, kind_of(fkv), elem_fmt(fkv), flags, marks};
     launch_pack(st, p, pack, 2);
     AttnFwd a = {};
     a.s = p.s; a.q = q; a.qb = d.qb; a.ql = d.ql; a.qh = d.qh; a.kq = kind_of(fq); a.fq = elem_fmt(fq); a.k = wk; a.v = wv; a.o = o; a.copy = o_copy; a.lse = lse;
     a.ko = kind_of(fout); a.fo = elem_fmt(fout); a.kc = kind_of(o_copy ? fcopy : fout); a.fc = elem_fmt(o_copy ? fcopy : fout);
     a.nbh = (int)p.nbh;
-    a.flags = flags; a.vsrc = v; a.vb = d.vb; a.vl = d.vl; a.vh = d.vh; a.kv = kind_of(fkv); a.fv = elem_fmt(fkv);
+    a.flags = flags; a.marks = marks;
     // The probabilities to 16 bits where an output's format keeps more than 8.  In the copy that the backward pass reads, what the rounding to 8 takes from
     // a row is common to all its gradients of scores (error of dq 2.6e-3 rather than 2.4e-3, 1.7e-3 of it its own rounding to bfloat16).
     if (fout != PNN_BF16 || (o_copy && fcopy != PNN_BF16)) launch_fwd<true>(st, p, a);
@@ -244,13 +245,14 @@ extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo
     uint4* const at = (uint4*)workspace;
     uint4 *wq = at, *wg = at + nq, *wqt = at + 2 * nq, *wgt = at + 3 * nq, *wk = at + 4 * nq, *wv = wk + nk, *wkt = wk + 2 * nk;
     float* const stats = (float*)(wk + 3 * nk);
-    int32_t* const flags = (int32_t*)(stats + p.nbh * p.s.qblocks * AT_STATS);
+    uint4* const marks = (uint4*)(stats + p.nbh * p.s.qblocks * AT_STATS);
+    int32_t* const flags = (int32_t*)(marks + p.nbh * p.s.qblocks * AT_MARKS);
     AttnPack pack = {};
     pack.B = (int)d.B; pack.HKV = (int)d.HKV; pack.D = (int)d.D;
-    pack.item[0] = {q, d.qb, d.ql, d.qh, p.s.rows, p.s.qblocks, wq, wqt, p.s.G, kind_of(fq), elem_fmt(fq), nullptr};
-    pack.item[1] = {d_o, d.qb, d.ql, d.qh, p.s.rows, p.s.qblocks, wg, wgt, p.s.G, kind_of(fd), elem_fmt(fd), flags};
-    pack.item[2] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, wkt, 1, kind_of(fkv), elem_fmt(fkv), nullptr};
-    pack.item[3] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, wv, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr};
+    pack.item[0] = {q, d.qb, d.ql, d.qh, p.s.rows, p.s.qblocks, wq, wqt, p.s.G, kind_of(fq), elem_fmt(fq), nullptr, nullptr};
+    pack.item[1] = {d_o, d.qb, d.ql, d.qh, p.s.rows, p.s.qblocks, wg, wgt, p.s.G, kind_of(fd), elem_fmt(fd), flags, marks};
+    pack.item[2] = {k, d.kb, d.kl, d.kh, p.s.LK, p.s.kblocks, wk, wkt, 1, kind_of(fkv), elem_fmt(fkv), nullptr, nullptr};
+    pack.item[3] = {v, d.vb, d.vl, d.vh, p.s.LK, p.s.kblocks, wv, nullptr, 1, kind_of(fkv), elem_fmt(fkv), nullptr, nullptr};
     launch_pack(st, p, pack, 4);
     if (d.LQ > 0) {
         AttnStats c = {};
@@ -262,7 +264,7 @@ extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo
     a.s = p.s; a.q = wq; a.g = wg; a.qt = wqt; a.gt = wgt; a.k = wk; a.v = wv; a.kt = wkt; a.stats = stats; a.dq = dq; a.dk = dk; a.dv = dv;
     a.kout = kind_of(fout); a.fout = elem_fmt(fout); a.nbh = (int)p.nbh;
     a.parts = dkv_parts(p); a.part = (float*)(flags + p.nbh * p.s.qblocks);
-    a.flags = flags; a.gsrc = d_o; a.gb = d.qb; a.gl = d.ql; a.gh = d.qh; a.kg = kind_of(fd); a.fg = elem_fmt(fd);
+    a.flags = flags; a.marks = marks;
     if (fout == PNN_BF16) launch_bwd<false>(st, p, a);
     else launch_bwd<true>(st, p, a);
     return hip_status(hipGetLastError());

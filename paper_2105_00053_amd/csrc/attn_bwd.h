@@ -25,11 +25,8 @@ struct AttnBwd {
     int kout;
     ElemFmt fout;
     int nbh;
-    const int32_t* flags;         // of d_o's blocks, and d_o itself for those
-    const void* gsrc;
-    int64_t gb, gl, gh;
-    int kg;
-    ElemFmt fg;
+    const int32_t* flags;         // of d_o's blocks
+    const uint4* marks;
     int parts;                    // workgroups to a tile of keys; each of them leaves its rows' sums in `part`, [part][batch, head][key][dK, dV][element]
     float* part;
 };
@@ -313,21 +310,22 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
     bool flagged = false;
     for (int n = lane; n < blocks && turn == 1; n += 64) flagged |= a.flags[rows0 + first + n] != 0;
     flagged = __any(flagged);
-    if (key >= s.LK) return;
-    AttnMarks marks = {};
+    AttnMarks<DB> marks = {};
     if (flagged)
-        for (int n = 0; n < blocks; ++n) {
-            if (!a.flags[rows0 + first + n]) continue;
-            for (int row = (first + n) * 32; row < (first + n) * 32 + 32 && row < s.rows; ++row) {
-                const int i = row / s.G, p = base + i;
-                if (at_sees(s, p, s.window ? p - s.window : -1, key))
-#pragma unroll 1
-                    for (int e = 0; e < 16 * DB; ++e) {
-                        const int d = (e >> 4) * 32 + at_row(e & 15, half);
-                        if (d < s.D) marks.add(e, load_value(a.gsrc, b * a.gb + i * a.gl + (hk * s.G + (row - i * s.G)) * a.gh + d, a.kg, a.fg));
-                    }
-            }
-        }
+        marks = at_marks<DB>(
+            a.flags + rows0, a.marks + rows0 * AT_MARKS, blocks, key < s.sinks, [&](int n) { return first + n; },
+            [&](int blk) {
+                const int p0 = base + blk * 32 / s.G, p1 = base + (blk * 32 + 31) / s.G;  // p1: the last row's position or more
+                const int low0 = s.window ? p0 - s.window : -1, low1 = s.window ? p1 - s.window : -1;
+                if (!(kw <= p1 && (kw + 31 > low0 || kw < s.sinks))) return AT_NONE;
+                if (kw + 31 > p0) return AT_EDGE;
+                return kw > low1 || kw + 31 < s.sinks ? AT_ALL : (kw + 31 <= low0 ? AT_SINKS : AT_EDGE);
+            },
+            [&](int row) {
+                const int p = base + row / s.G;
+                return row < s.rows && at_sees(s, p, s.window ? p - s.window : -1, key);
+            });
+    if (key >= s.LK) return;
     const int64_t at = a.parts > 1 ? (((share * (int64_t)a.nbh + bh) * s.LK + key) * 2 + turn) * s.D : (((int64_t)b * s.LK + key) * s.HKV + hk) * s.D;
     void* const out = a.parts > 1 ? a.part : (turn ? a.dv : a.dk);
     const int kind = a.parts > 1 ? KIND_F32 : a.kout;
@@ -337,7 +335,7 @@ __global__ __launch_bounds__(128 * at_parallel(DB), DB <= 2 ? 2 : 1) void attn_d
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             dk[d][r] *= up;
-            if (flagged) dk[d][r] = marks.apply(16 * d + r, dk[d][r]);
+            if (flagged) dk[d][r] = at_marked(dk[d][r], marks.pos[d], marks.neg[d], marks.nan[d], at_row(r, half));
         }
         at_eights(dk[d], half, [&](int e, const float (&v)[8]) { at_store8(out, at + d * 32 + e, s.D - d * 32 - e, kind, a.fout, v); });
     }

@@ -8,7 +8,7 @@
 //    8 + 4 (l / 32) + i - 4: the order in which a lane's result registers hold them.  So the probabilities of one product are operands
 //    of the next as they come out of it, rounded in place, without any exchange between lanes.  They hold zeros in place of infinities and
 //    NaN: a probability of zero times one of those would reach rows that do not see it.  Where they matter the kernels look
-//    them up (AttnMarks) in blocks that the packing kernel flagged.
+//    them up (AttnMarks) in what the packing kernel notes of the blocks that hold any.
 // Formats that bfloat16 holds exactly make every product exact; decoding in the kernels themselves would cost 14 vector operations an element
 // and tile, four times what the matrix instructions of a tile of 128 x 64 take, so each operand is decoded once.
 // The query heads that share a key head are one operand: row r = position * G + head within the group.
@@ -68,6 +68,10 @@ __device__ __forceinline__ int at_snake(int i, int n, int nbh) {
     return (turn & 1) ? first + size - 1 - (i - first) : i;
 }
 
+// What a block of 32 rows holds that is not finite: for each row, and last for all of them together, one bit an element of a head in three
+// masks of 128 (+infinity, -infinity, NaN).
+constexpr int AT_MARKS = 33 * 3;
+
 struct AttnPackItem {
     const void* src;
     int64_t sb, sl, sh;   // strides: batch, position, head
@@ -76,6 +80,7 @@ struct AttnPackItem {
     int G, kind;
     ElemFmt f;
     int32_t* flags;       // one per block, may be null: whether it holds anything that is not finite
+    uint4* marks;         // AT_MARKS per block, written where it does
 };
 
 struct AttnPack {
@@ -129,6 +134,29 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnPack a) {
     const bool any = __syncthreads_or(odd);
     const int64_t bh = (int64_t)b * a.HKV + hk;
     if (p.flags && t == 0) p.flags[bh * p.blocks + blk] = any;
+    if (p.flags && any) {
+        // a row to a thread and word of 32 elements, then the columns' together
+        uint32_t* const m = (uint32_t*)(p.marks + (bh * p.blocks + blk) * AT_MARKS);
+        for (int c = t; c < 32 * 4; c += 256) {
+            const int r = c >> 2, d = c & 3;
+            uint32_t pos = 0, neg = 0, nan = 0;
+            for (int e = 0; d < DB && e < 32; ++e) {
+                const uint32_t x = tile[r][d * 32 + e], bit = (x & 0x7F80u) == 0x7F80u ? 1u << e : 0u;
+                nan |= x & 0x7Fu ? bit : 0u;
+                neg |= (x & 0x807Fu) == 0x8000u ? bit : 0u;
+                pos |= (x & 0x807Fu) == 0u ? bit : 0u;
+            }
+            m[r * 12 + d] = pos;
+            m[r * 12 + 4 + d] = neg;
+            m[r * 12 + 8 + d] = nan;
+        }
+        __syncthreads();
+        if (t < 12) {
+            uint32_t w = 0;
+            for (int r = 0; r < 32; ++r) w |= m[r * 12 + t];
+            m[32 * 12 + t] = w;
+        }
+    }
     if (p.row_frags)
         for (int c = t; c < KS * 64; c += 256) {
             const int l = c & 63, r = l & 31, d = (c >> 6) * 16 + 8 * (l >> 5);
@@ -225,21 +253,70 @@ __device__ __forceinline__ at_v8b at_scaled(uint4 v, float c) {
     return q;
 }
 
-// What infinities and NaN that a result's row sees make of it; the packed operand held zeros in their place.
+// What infinities and NaN that a result's row (its key, in the backward pass) sees make of it; the packed operand held zeros in their place.
+template <int DB>
 struct AttnMarks {
-    uint64_t pos, neg, nan;  // one bit a result register
-    __device__ __forceinline__ void add(int bit, float v) {
-        const uint64_t m = (uint64_t)1 << bit;
-        const bool inf = v - v != 0.f && v == v;
-        pos |= inf && v > 0.f ? m : 0;
-        neg |= inf && v < 0.f ? m : 0;
-        nan |= v != v ? m : 0;
+    uint32_t pos[DB], neg[DB], nan[DB];  // one bit an element of a head
+    __device__ __forceinline__ void add(const uint32_t (&p)[4], const uint32_t (&n)[4], const uint32_t (&q)[4], bool see) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            pos[d] |= see ? p[d] : 0u;
+            neg[d] |= see ? n[d] : 0u;
+            nan[d] |= see ? q[d] : 0u;
+        }
     }
-    __device__ __forceinline__ float apply(int bit, float v) const {
-        const bool p = (pos >> bit) & 1u, n = (neg >> bit) & 1u;
-        if (((nan >> bit) & 1u) || (p && n) || v != v) return f32_of_bits(0x7FC00000u);
-        return p ? f32_of_bits(0x7F800000u) : (n ? f32_of_bits(0xFF800000u) : v);
+    // the three masks of a block's row, as the packing kernel left them
+    __device__ __forceinline__ void add(const uint4* m, bool see) {
+        uint32_t w[3][4];
+        __builtin_memcpy(w, m, sizeof w);
+        add(w[0], w[1], w[2], see);
+    }
+    // the marks of all lanes together, in every lane; `see`: whether the lane's row has them
+    __device__ __forceinline__ void add_all_lanes(const AttnMarks& o, bool see) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            uint32_t w[3] = {o.pos[d], o.neg[d], o.nan[d]};
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {
+                for (int m = 32; m >= 1; m >>= 1) w[x] |= (uint32_t)__shfl_xor((int)w[x], m, 64);
+                w[x] = see ? w[x] : 0u;
+            }
+            pos[d] |= w[0];
+            neg[d] |= w[1];
+            nan[d] |= w[2];
+        }
     }
 };
+// v, given the three masks' words that its bit is in
+__device__ __forceinline__ float at_marked(float v, uint32_t pos, uint32_t neg, uint32_t nan, int bit) {
+    const bool p = (pos >> bit) & 1u, n = (neg >> bit) & 1u;
+    if (((nan >> bit) & 1u) || (p && n) || v != v) return f32_of_bits(0x7FC00000u);
+    return p ? f32_of_bits(0x7F800000u) : (n ? f32_of_bits(0xFF800000u) : v);
+}
+
+// How the 32 rows of a wave see a block of 32 of the other side: not at all, all of them all of it, only where `sink` says so, or each pair for itself.
+enum AttnSight { AT_NONE, AT_ALL, AT_SINKS, AT_EDGE };
+
+// Marks of `count` blocks for a wave's rows; all its lanes call.  Blocks seen alike are taken one to a lane, those at the mask's edges row by row: as
+// many as the mask has edges, whatever the length.
+template <int DB, class Block, class Sight, class Sees>
+__device__ __forceinline__ AttnMarks<DB> at_marks(const int32_t* flags, const uint4* marks, int count, bool sink, Block block, Sight sight, Sees sees) {
+    AttnMarks<DB> own = {}, all = {}, sinks = {};
+    const int lane = threadIdx.x & 63;
+    for (int n0 = 0; n0 < count; n0 += 64) {
+        const bool in = n0 + lane < count;
+        const int blk = in ? block(n0 + lane) : 0, how = in && flags[blk] ? sight(blk) : AT_NONE;
+        if (how == AT_ALL) all.add(marks + (int64_t)blk * AT_MARKS + 96, true);
+        if (how == AT_SINKS) sinks.add(marks + (int64_t)blk * AT_MARKS + 96, true);
+        for (uint64_t edge = __ballot(how == AT_EDGE); edge; edge &= edge - 1) {
+            const int at = block(n0 + __builtin_ctzll(edge));
+#pragma unroll 4
+            for (int r = 0; r < 32; ++r) own.add(marks + (int64_t)at * AT_MARKS + 3 * r, sees(at * 32 + r));
+        }
+    }
+    own.add_all_lanes(all, true);
+    own.add_all_lanes(sinks, sink);
+    return own;
+}
 
 }  // namespace pnn

@@ -27,11 +27,8 @@ struct AttnFwd {
     int ko, kc;
     ElemFmt fo, fc;
     int nbh;  // B * HKV
-    const int32_t* flags;  // of v's blocks, and v itself for those
-    const void* vsrc;
-    int64_t vb, vl, vh;
-    int kv;
-    ElemFmt fv;
+    const int32_t* flags;  // of v's blocks
+    const uint4* marks;
 };
 
 // The tiles of TK keys that rows of positions p0 .. p1 see: sinks first, then the window.
@@ -167,20 +164,17 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
     bool flagged = false;
     for (int n = lane; n < tiles.count; n += 64) flagged |= (flags[2 * tiles.at(n)] | flags[2 * tiles.at(n) + 1]) != 0;
     flagged = __any(flagged);
-    if (!live) return;
-    AttnMarks marks = {};
+    AttnMarks<DB> marks = {};
     if (flagged)
-        for (int n = 0; n < 2 * tiles.count; ++n) {
-            const int blk = 2 * tiles.at(n >> 1) + (n & 1);
-            if (!flags[blk]) continue;
-            for (int j = blk * 32; j < blk * 32 + 32; ++j)
-                if (at_sees(s, p, low, j))
-#pragma unroll 1
-                    for (int e = 0; e < 16 * DB; ++e) {
-                        const int d = (e >> 4) * 32 + at_row(e & 15, half);
-                        if (d < s.D) marks.add(e, load_value(a.vsrc, b * a.vb + j * a.vl + hk * a.vh + d, a.kv, a.fv));
-                    }
-        }
+        marks = at_marks<DB>(
+            flags, a.marks + (int64_t)bh * s.kblocks * AT_MARKS, 2 * tiles.count, false, [&](int n) { return 2 * tiles.at(n >> 1) + (n & 1); },
+            [&](int blk) {
+                const int key0 = blk * 32;
+                if (!(key0 <= wp1 && (key0 + 31 > wlow0 || key0 < s.sinks))) return AT_NONE;
+                return key0 + 31 <= wp0 && (key0 > wlow1 || key0 + 31 < s.sinks) ? AT_ALL : AT_EDGE;
+            },
+            [&](int key) { return at_sees(s, p, low, key); });
+    if (!live) return;
     const int h = hk * s.G + (row - i * s.G);
     if (a.lse && half == 0) a.lse[((int64_t)b * s.HKV * s.G + h) * s.LQ + i] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
     const int64_t at = (((int64_t)b * s.LQ + i) * (s.HKV * s.G) + h) * s.D;
@@ -190,7 +184,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnFwd a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             o[d][r] *= up;
-            if (flagged) o[d][r] = marks.apply(16 * d + r, o[d][r]);
+            if (flagged) o[d][r] = at_marked(o[d][r], marks.pos[d], marks.neg[d], marks.nan[d], at_row(r, half));
         }
         at_eights(o[d], half, [&](int e, const float (&v)[8]) {
             e += d * 32;

@@ -243,19 +243,40 @@ __global__ __launch_bounds__(256, sizeof(typename Raw<K>::T) == 1 ? 3 : 2) void 
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (__any(flagged != 0)) {
-        AttnMarks marks = {};
+        // the wave's tiles once more, an element of a value to a lane
+        AttnMarks<DB> marks = {};
         for (int n = begin + w; n < end; n += 4)
-            for (int j = tiles.at(n) * 32; j < tiles.at(n) * 32 + 32; ++j)
-                if (at_sees(s, p, low, j))
-#pragma unroll 1
-                    for (int e = 0; e < 4 * NV; ++e) {
-                        const int d = NV * (4 * quarter + (e & 3)) + (e >> 2);
-                        if (d < s.D) marks.add(e, value_of<K>(vsrc[j * a.vl + d], a.fkv));
+#pragma unroll 4
+            for (int r = 0; r < 32; ++r) {
+                const int key = tiles.at(n) * 32 + r;
+                const T* const src = vsrc + (int64_t)(key < keys ? key : keys - 1) * a.vl;
+                uint32_t m[3][4] = {};
+#pragma unroll
+                for (int x = 0; x < (DB + 1) / 2; ++x) {
+                    const int d = 64 * x + lane;
+                    const float v = d < s.D ? value_of<K>(src[d], a.fkv) : 0.f;
+                    const uint64_t b[3] = {__ballot(v == inf), __ballot(v == -inf), __ballot(v != v)};
+#pragma unroll
+                    for (int y = 0; y < 3; ++y) {
+                        m[y][2 * x] = (uint32_t)b[y];
+                        m[y][2 * x + 1] = (uint32_t)(b[y] >> 32);
                     }
+                }
+                marks.add(m[0], m[1], m[2], at_sees(s, p, low, key));
+            }
+        // the lane's elements NV (4 quarter + r) + x lie in one word
+        const int word = NV * quarter / 8, from = NV * 4 * quarter & 31;
+        uint32_t pos = 0, neg = 0, nan = 0;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            pos = word == d ? marks.pos[d] : pos;
+            neg = word == d ? marks.neg[d] : neg;
+            nan = word == d ? marks.nan[d] : nan;
+        }
 #pragma unroll
         for (int x = 0; x < NV; ++x)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[x][r] = marks.apply(4 * x + r, o[x][r]);
+            for (int r = 0; r < 4; ++r) o[x][r] = at_marked(o[x][r], pos, neg, nan, from + NV * r + x);
     }
 
     // join the waves: a common reference, then through LDS, [wave][block][element row][column]
