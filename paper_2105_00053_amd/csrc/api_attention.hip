@@ -15,7 +15,7 @@ inline int desc_status(const pnn_attention_desc* d) {
     if ((d->HKV == 0) != (d->HQ == 0) || (d->HKV > 0 && d->HQ % d->HKV != 0)) return PNN_EINVAL;
     if (!(d->scale > -3.4028235e38f && d->scale < 3.4028235e38f)) return PNN_EINVAL;
     if (d->qb < 0 || d->ql < 0 || d->qh < 0 || d->kb < 0 || d->kl < 0 || d->kh < 0 || d->vb < 0 || d->vl < 0 || d->vh < 0) return PNN_EINVAL;
-    // rows of a group and keys are counted in 32 bits, workgroups by the grid's limits
+    // rows of a group and keys are counted in 32 bits, workgroups by the grid's limits (along x: see launches())
     const int64_t most = ((int64_t)1 << 31) - 128;
     if (d->D > 128 || d->LQ > most || d->LK > most || d->HQ >= 65536 || d->B >= 16384) return PNN_EUNSUPPORTED;
     if (d->HKV > 0 && d->LQ * (d->HQ / d->HKV) > most) return PNN_EUNSUPPORTED;
@@ -100,6 +100,13 @@ int64_t dkv_part_bytes(const Plan& p) {
     return parts > 1 ? parts * p.nbh * p.s.LK * 2 * p.s.D * 4 : 0;
 }
 
+// whether every launch's threads can be counted
+bool launches(int which, const Plan& p) {
+    const int64_t most = most_workgroups(256);
+    if (p.nbh * (p.s.qblocks / 4) > most || p.s.kblocks > most) return false;
+    return which == 0 || (p.s.qblocks <= most && p.nbh * (p.s.kblocks / 2) * dkv_parts(p) <= most_workgroups(128 * at_parallel(p.db)));
+}
+
 void launch_pack(hipStream_t st, const Plan& p, const AttnPack& a, int items) {
     int64_t blocks = 0;
     for (int i = 0; i < items; ++i) blocks = a.item[i].blocks > blocks ? a.item[i].blocks : blocks;
@@ -164,6 +171,7 @@ extern "C" size_t posit_attention_workspace(int which, int fkv, const pnn_attent
     const Plan p = make_plan(*desc);
     const TokenPlan t = token_plan(p.s, desc->B);
     if (which == 0 && t.use) return (size_t)t.bytes;
+    if (!launches(which, p)) return 0;
     if (which == 0) return (size_t)(2 * p.k_bytes + p.nbh * p.s.kblocks * (AT_MARKS * 16 + 4));
     return (size_t)(4 * p.q_bytes + 3 * p.k_bytes + p.nbh * p.s.qblocks * (AT_STATS * 4 + AT_MARKS * 16 + 4) + dkv_part_bytes(p));
 }
@@ -178,14 +186,15 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     const pnn_attention_desc& d = *desc;
     if (d.B == 0 || d.HQ == 0 || d.LQ == 0 || d.D == 0) return PNN_OK;
     if (!q || !o || (d.LK > 0 && (!k || !v))) return PNN_EINVAL;
+    Plan p = make_plan(d);
+    p.s.lens = lens;
+    const TokenPlan tp = token_plan(p.s, d.B);
+    if (!tp.use && !launches(0, p)) return PNN_EUNSUPPORTED;
     const size_t need = posit_attention_workspace(0, fkv, desc);
     if (need > 0 && (!workspace || workspace_bytes < need)) return PNN_EWORKSPACE;
     if (need > 0 && !aligned(workspace, 16)) return PNN_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
-    Plan p = make_plan(d);
-    p.s.lens = lens;
-    const TokenPlan tp = token_plan(p.s, d.B);
     if (tp.use) {
         AttnToken a = {};
         a.s = p.s; a.q = q; a.k = k; a.v = v;
@@ -234,13 +243,14 @@ extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo
     const pnn_attention_desc& d = *desc;
     if (d.B == 0 || d.HQ == 0 || d.D == 0 || (d.LQ == 0 && d.LK == 0)) return PNN_OK;
     if ((d.LQ > 0 && (!d_o || !q || !o || !lse || !dq)) || (d.LK > 0 && (!k || !v || !dk || !dv))) return PNN_EINVAL;
+    Plan p = make_plan(d);
+    p.s.lens = lens;
+    if (!launches(1, p)) return PNN_EUNSUPPORTED;
     const size_t need = posit_attention_workspace(1, fkv, desc);
     if (need > 0 && (!workspace || workspace_bytes < need)) return PNN_EWORKSPACE;
     if (need > 0 && !aligned(workspace, 16)) return PNN_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
-    Plan p = make_plan(d);
-    p.s.lens = lens;
     const int64_t nq = p.q_bytes / 16, nk = p.k_bytes / 16;
     uint4* const at = (uint4*)workspace;
     uint4 *wq = at, *wg = at + nq, *wqt = at + 2 * nq, *wgt = at + 3 * nq, *wk = at + 4 * nq, *wv = wk + nk, *wkt = wk + 2 * nk;

@@ -26,6 +26,7 @@ struct LogprobFwd {
     float tau;
     int top, kind;
     ElemFmt f;
+    int64_t row0;        // the launch's first row
     int64_t span;        // logits of a part, a multiple of 2048
     int parts;
     float4* part_stats;  // for more than one part: maximum, two sums, "holds a NaN or +inf"
@@ -209,8 +210,9 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     __shared__ LogprobTop sh;
     __shared__ uint32_t hist[K == KIND_POSIT_U8 ? 256 * LP_COPIES : 1];
     const int t = threadIdx.x;
-    const int64_t row = blockIdx.x / (unsigned)a.parts;
-    const int p = blockIdx.x - (unsigned)row * a.parts;
+    const unsigned nth = blockIdx.x / (unsigned)a.parts;
+    const int64_t row = a.row0 + nth;
+    const int p = blockIdx.x - nth * a.parts;
     const int64_t begin = p * a.span;
     const int n = (int)(a.vocab - begin < a.span ? a.vocab - begin : a.span), vectors = n / 8, rest = n - vectors * 8;
     const char* const src = (const char*)a.z + (row * a.ldz + begin) * B;
@@ -421,7 +423,7 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
 __global__ __launch_bounds__(256) void logprob_join_kernel(LogprobFwd a) {
     __shared__ float part[12];
     __shared__ LogprobTop sh;
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const int t = threadIdx.x;
     const float inf = f32_of_bits(0x7F800000u);
     const float4* const st = a.part_stats + row * a.parts;
@@ -468,6 +470,7 @@ struct LogprobBwd {
     float tau;
     int kg;
     ElemFmt fz, fg;
+    int64_t row0;  // the launch's first row
     int64_t span;
     int parts;
 };
@@ -477,8 +480,9 @@ struct LogprobBwd {
 template <int K>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwd a) {
     const int t = threadIdx.x;
-    const int64_t row = blockIdx.x / (unsigned)a.parts;
-    const int64_t begin = (blockIdx.x - row * a.parts) * a.span, end = begin + a.span < a.vocab ? begin + a.span : a.vocab;
+    const unsigned nth = blockIdx.x / (unsigned)a.parts;
+    const int64_t row = a.row0 + nth;
+    const int64_t begin = (int64_t)(blockIdx.x - nth * a.parts) * a.span, end = begin + a.span < a.vocab ? begin + a.span : a.vocab;
     const float inf = f32_of_bits(0x7F800000u), lse = a.lse[row];
     const int32_t y = a.g_lp ? a.target[row] : -1;
     const float gl = y < 0 ? 0.f : (y >= a.vocab ? f32_of_bits(0x7FC00000u) : a.g_lp[row]) * a.tau;
@@ -535,20 +539,22 @@ extern "C" int posit_token_logprob_fwd(void* stream, int fz, int64_t rows, int64
                                        void* workspace, size_t workspace_bytes) {
     if (rows < 0 || vocab < 0 || ldz < vocab || top < 0 || !(inv_temperature > 0.f && inv_temperature <= 3.4028235e38f)) return PNN_EINVAL;
     if (const int s = element_status(fz)) return s;
-    if (top > 64 || vocab >= ((int64_t)1 << 31)) return PNN_EUNSUPPORTED;
+    if (top > 64 || vocab >= ((int64_t)1 << 31) || rows >= ((int64_t)1 << 31)) return PNN_EUNSUPPORTED;
     if (rows == 0 || vocab == 0) return PNN_OK;
     if (!logits || (logprob && !targets) || (top > 0 && (!top_logprob || !top_index)) || (!logprob && !lse && !entropy && top == 0)) return PNN_EINVAL;
     const int64_t span = logprob_span(fz, rows, vocab), parts = (vocab + span - 1) / span;
-    if (rows >= ((int64_t)1 << 31) / parts) return PNN_EUNSUPPORTED;  // workgroups of one launch
     const size_t need = posit_token_logprob_workspace(fz, rows, vocab, top);
     if (need > 0 && (!workspace || workspace_bytes < need)) return PNN_EWORKSPACE;
     if (need > 0 && !aligned(workspace, 16)) return PNN_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
-    LogprobFwd a = {logits, targets, logprob, lse, entropy, top_logprob, top_index, vocab, ldz, inv_temperature, top, kind_of(fz), elem_fmt(fz), span, (int)parts,
+    LogprobFwd a = {logits, targets, logprob, lse, entropy, top_logprob, top_index, vocab, ldz, inv_temperature, top, kind_of(fz), elem_fmt(fz), 0, span, (int)parts,
                     (float4*)workspace, (lp_key*)((char*)workspace + rows * parts * 16)};
-    PNN_DISPATCH_KIND(a.kind, hipLaunchKernelGGL(logprob_part_kernel<K>, dim3((unsigned)(rows * parts)), dim3(256), 0, st, a))
-    if (parts > 1) hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+    for (const int64_t most = most_workgroups(256) / parts; a.row0 < rows; a.row0 += most) {
+        const int64_t n = rows - a.row0 < most ? rows - a.row0 : most;
+        PNN_DISPATCH_KIND(a.kind, hipLaunchKernelGGL(logprob_part_kernel<K>, dim3((unsigned)(n * parts)), dim3(256), 0, st, a))
+        if (parts > 1) hipLaunchKernelGGL(logprob_join_kernel, dim3((unsigned)n), dim3(256), 0, st, a);
+    }
     return hip_status(hipGetLastError());
 }
 
@@ -558,15 +564,17 @@ extern "C" int posit_token_logprob_bwd(void* stream, int fz, int fg, int64_t row
     if (rows < 0 || vocab < 0 || ldz < vocab || ldg < vocab || !(inv_temperature > 0.f && inv_temperature <= 3.4028235e38f)) return PNN_EINVAL;
     for (int f : {fz, fg})
         if (const int s = element_status(f)) return s;
-    if (vocab >= ((int64_t)1 << 31)) return PNN_EUNSUPPORTED;
+    if (vocab >= ((int64_t)1 << 31) || rows >= ((int64_t)1 << 31)) return PNN_EUNSUPPORTED;
     if (rows == 0 || vocab == 0) return PNN_OK;
     if (!logits || !lse || !dlogits || (g_logprob && !targets) || (g_entropy && !entropy)) return PNN_EINVAL;
     // four vectors to a thread keep the next load in flight; parts of one where rows are few
     const int64_t span = rows * ((vocab + 8191) / 8192) >= 1024 ? 8192 : 2048, parts = (vocab + span - 1) / span;
-    if (rows >= ((int64_t)1 << 31) / parts) return PNN_EUNSUPPORTED;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
-    const LogprobBwd a = {logits, targets, lse, entropy, g_logprob, g_entropy, dlogits, rows, vocab, ldz, ldg, inv_temperature, kind_of(fg), elem_fmt(fz), elem_fmt(fg), span, (int)parts};
-    PNN_DISPATCH_KIND(kind_of(fz), hipLaunchKernelGGL(logprob_bwd_kernel<K>, dim3((unsigned)(rows * parts)), dim3(256), 0, st, a))
+    LogprobBwd a = {logits, targets, lse, entropy, g_logprob, g_entropy, dlogits, rows, vocab, ldz, ldg, inv_temperature, kind_of(fg), elem_fmt(fz), elem_fmt(fg), 0, span, (int)parts};
+    for (const int64_t most = most_workgroups(256) / parts; a.row0 < rows; a.row0 += most) {
+        const int64_t n = rows - a.row0 < most ? rows - a.row0 : most;
+        PNN_DISPATCH_KIND(kind_of(fz), hipLaunchKernelGGL(logprob_bwd_kernel<K>, dim3((unsigned)(n * parts)), dim3(256), 0, st, a))
+    }
     return hip_status(hipGetLastError());
 }

@@ -22,6 +22,7 @@ struct NormFwd {
     void *res_out, *y;
     float *scale, *rstd;
     int64_t rows, cols, ldx, ldr, ldo, ldy;
+    int64_t row0;  // of a launch with a row to a workgroup
     float eps;
     int kx, kr, kw, ky;
     ElemFmt fx, fr, fw, fy;
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T
 __global__ __launch_bounds__(256) void rmsnorm_fwd_kernel(NormFwd a) {
     __shared__ float part[4];
     __shared__ uint32_t partu[4];
-    const int64_t r = blockIdx.x;
+    const int64_t r = a.row0 + blockIdx.x;
     const int t = threadIdx.x;
     const void* h = a.res ? a.res_out : a.x;
     const int kh = a.res ? a.kr : a.kx;
@@ -206,6 +207,7 @@ struct NormBwd {
     const float* rstd;
     void *dx, *dw;
     int64_t rows, cols, lddy, ldh, lddr, lddx;
+    int64_t row0;  // of a launch with a row to a workgroup
     int kd, kh, kw, kr, kx, kdw;
     ElemFmt fd, fh, fw, fr, fx, fdw;
     float* part;
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(1024) void rmsnorm_dw_join_kernel(const float* part
 // Longer rows.
 __global__ __launch_bounds__(256) void rmsnorm_bwd_kernel(NormBwd a) {
     __shared__ float part[4];
-    const int64_t r = blockIdx.x;
+    const int64_t r = a.row0 + blockIdx.x;
     const int t = threadIdx.x;
     float s = 0.f;
     for (int64_t j = t; j < a.cols; j += 256)
@@ -422,13 +424,16 @@ extern "C" int posit_rmsnorm_fwd(void* stream, int fx, int fres, int fw, int fy,
     if (!x || !w || !y || (res && !res_out)) return PNN_EINVAL;
     if (rows >= ((int64_t)1 << 31) || cols >= ((int64_t)1 << 31)) return PNN_EUNSUPPORTED;
     discard_stale_hip_error();
-    NormFwd a = {x, res, w, res_out, y, scale, rstd, rows, cols, ldx, ldr, ldo, ldy, eps, kind_of(fx), res ? kind_of(fres) : 0, kind_of(fw), kind_of(fy),
+    NormFwd a = {x, res, w, res_out, y, scale, rstd, rows, cols, ldx, ldr, ldo, ldy, 0, eps, kind_of(fx), res ? kind_of(fres) : 0, kind_of(fw), kind_of(fy),
                  elem_fmt(fx), elem_fmt(res ? fres : fx), elem_fmt(fw), elem_fmt(fy)};
     hipStream_t st = (hipStream_t)stream;
     const NormPlan p = norm_plan(rows, cols, NORM_FWD_WAVES);
     if (p.rows) {
         PNN_DISPATCH_KIND(a.kx, launch_fwd_rows<K>(st, p, a))
-    } else hipLaunchKernelGGL(rmsnorm_fwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+    } else {
+        for (const int64_t most = most_workgroups(256); a.row0 < rows; a.row0 += most)
+            hipLaunchKernelGGL(rmsnorm_fwd_kernel, dim3((unsigned)(rows - a.row0 < most ? rows - a.row0 : most)), dim3(256), 0, st, a);
+    }
     return hip_status(hipGetLastError());
 }
 
@@ -450,7 +455,7 @@ extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres
     const size_t need = dw ? posit_rmsnorm_bwd_workspace(rows, cols) : 0;
     if (need > 0 && (!workspace || workspace_bytes < need)) return PNN_EWORKSPACE;
     if (need > 0 && !aligned(workspace, 16)) return PNN_EINVAL;
-    NormBwd a = {dy, h, w, dres, rstd, dx, dw, rows, cols, lddy, ldh, lddr, lddx, kind_of(fd), kind_of(fh), kind_of(fw), kind_of(dres ? fdres : fd), kind_of(fdx),
+    NormBwd a = {dy, h, w, dres, rstd, dx, dw, rows, cols, lddy, ldh, lddr, lddx, 0, kind_of(fd), kind_of(fh), kind_of(fw), kind_of(dres ? fdres : fd), kind_of(fdx),
                  kind_of(dw ? fdw : fd), elem_fmt(fd), elem_fmt(fh), elem_fmt(fw), elem_fmt(dres ? fdres : fd), elem_fmt(fdx), elem_fmt(dw ? fdw : fd), (float*)workspace};
     hipStream_t st = (hipStream_t)stream;
     const NormPlan p = norm_plan(rows, cols, NORM_BWD_WAVES);
@@ -458,7 +463,8 @@ extern "C" int posit_rmsnorm_bwd(void* stream, int fd, int fh, int fw, int fdres
         PNN_DISPATCH_KIND(a.kd, launch_bwd_rows_of<K>(st, p, a))
         if (dw) hipLaunchKernelGGL(rmsnorm_dw_join_kernel, dim3((unsigned)((cols + 31) / 32)), dim3(1024), 0, st, a.part, (int)p.groups, cols, dw, a.kdw, a.fdw);
     } else {
-        hipLaunchKernelGGL(rmsnorm_bwd_kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+        for (const int64_t most = most_workgroups(256); a.row0 < rows; a.row0 += most)
+            hipLaunchKernelGGL(rmsnorm_bwd_kernel, dim3((unsigned)(rows - a.row0 < most ? rows - a.row0 : most)), dim3(256), 0, st, a);
         if (dw) hipLaunchKernelGGL(rmsnorm_dw_kernel, dim3((unsigned)((cols + 255) / 256)), dim3(256), 0, st, a);
     }
     return hip_status(hipGetLastError());

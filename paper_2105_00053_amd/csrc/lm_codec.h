@@ -27,6 +27,9 @@ inline ElemFmt elem_fmt(int f) {
     return e;
 }
 
+// Threads of a launch along x are counted in 32 bits: of more, some workgroups run and no error is reported.  Most workgroups of that many threads:
+constexpr int64_t most_workgroups(int threads) { return 0xFFFFFFFFll / threads; }
+
 PNN_HD float f32_of_bits(uint32_t b) { return __builtin_bit_cast(float, b); }
 PNN_HD uint32_t bits_of_f32(float v) { return __builtin_bit_cast(uint32_t, v); }
 

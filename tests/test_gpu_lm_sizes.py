@@ -27,3 +27,18 @@ def test_windows_and_sinks_beyond_the_cache(b, lq, lk, hq, hkv, d):
     some = run(100, lk)
     for sinks in (2 ** 31, MOST - 200, MOST):
         assert all(torch.equal(x, y) for x, y in zip(run(100, sinks), some)), sinks
+
+
+def test_more_rows_of_logits_than_a_launch_counts():
+    """Above 2^32 threads, 2^24 workgroups of 256, a launch leaves workgroups out without an error: the rows go in two."""
+    rows = 2 ** 24 + 5
+    z = torch.tensor([[0x40, 0x30, 0x40]], dtype=torch.uint8, device="cuda")
+    targets = torch.tensor([1], dtype=torch.int32, device="cuda")
+    g = torch.ones(1, device="cuda")
+    one = pn.posit_token_logprob_fwd(z, targets, "p8", top=1)
+    many = pn.posit_token_logprob_fwd(z.repeat(rows, 1), targets.repeat(rows), "p8", top=1)
+    for a, b in zip(one, many):
+        assert (b == a).all()
+    want = pn.posit_token_logprob_bwd(z, targets, one[1], one[2], g, g, "p8", "bf16")
+    got = pn.posit_token_logprob_bwd(z.repeat(rows, 1), targets.repeat(rows), many[1], many[2], g.repeat(rows), g.repeat(rows), "p8", "bf16")
+    assert (got == want).all()
