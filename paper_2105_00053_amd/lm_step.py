@@ -67,7 +67,8 @@ def gradients(net, tokens, targets, loss_scale=64.0):
     x, y1, rstd1, qkv = _project(net, tokens)
     q, k, v = net.split(qkv, b, l)
     how = dict(window=net.window, sinks=net.sinks)
-    o, lse, _ = lm.posit_attention_fwd(q, k, v, fc, fc, fc, **how)
+    # the products read o as it is; the backward pass takes rowsum(dO * o) from a copy in binary32, since all score gradients of a row share its error
+    o, lse, o_copy = lm.posit_attention_fwd(q, k, v, fc, fc, fc, fcopy="f32", **how)
     h, y2, rstd2, logits = _read_out(net, x, o.view(b * l, -1))
     targets = targets.reshape(-1)
     logprob, z_lse, entropy, _, _ = lm.posit_token_logprob_fwd(logits, targets, fl)
@@ -78,7 +79,7 @@ def gradients(net, tokens, targets, loss_scale=64.0):
     dh, dnorm2 = lm.posit_rmsnorm_bwd(pn.posit_gemm(dz, net.copies[2], fc, fc), h, net.norms[1], rstd2, fc, fm, fm, fc, fm)
     dout = pn.posit_gemm(dh, o.view(b * l, -1), fc, fm, trans_a=True)
     do = pn.posit_gemm(dh, net.copies[1], fc, fc).view(o.shape)
-    dqkv = torch.cat([_movable(t) for t in lm.posit_attention_bwd(do, q, k, v, o, lse, fc, fc, fc, fc, fc, **how)], dim=2).view(b * l, -1)
+    dqkv = torch.cat([_movable(t) for t in lm.posit_attention_bwd(do, q, k, v, o_copy, lse, fc, fc, fc, "f32", fc, **how)], dim=2).view(b * l, -1)
     dw = pn.posit_gemm(dqkv, y1, fc, fm, trans_a=True)
     _, dnorm1 = lm.posit_rmsnorm_bwd(pn.posit_gemm(dqkv, net.copies[0], fc, fc), x, net.norms[0], rstd1, fc, fm, fm, fc, fm)
     return logprob.view(b, l), [dw, dout, dhead], [dnorm1, dnorm2]
