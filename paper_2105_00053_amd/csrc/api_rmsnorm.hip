@@ -7,14 +7,16 @@
 
 namespace pnn {
 
-// The power of two that brings a row's largest magnitude (its binary32 word) into [4, 8), and the one that undoes it.  True, with NaN
-// for the first, where the row holds a NaN or an infinity.
-__device__ __forceinline__ bool norm_scale(uint32_t top, float& up, float& down) {
+// The power of two that brings a row's largest magnitude (its binary32 word) into [4, 8), as two factors, since it is up to 2^151 where that magnitude is
+// a subnormal number (`more` is 1 unless it is below 2^-125), and `rstd` times its inverse.  NaN for the first and the last where the row holds a NaN or an
+// infinity.
+__device__ __forceinline__ void norm_scale(uint32_t top, float rstd, float& up, float& more, float& scale) {
+    const float nan = f32_of_bits(0x7FC00000u);
     const bool bad = top >= 0x7F800000u;
-    const int e = top == 0 ? 2 : ((top >> 23) ? (int)(top >> 23) - 127 : -118 - clz32(top));
-    up = bad ? f32_of_bits(0x7FC00000u) : ldexpf(1.f, 2 - e);
-    down = ldexpf(1.f, e - 2);
-    return bad;
+    const int e = top == 0 ? 2 : ((top >> 23) ? (int)(top >> 23) - 127 : -118 - clz32(top)), k = e < -125 ? 127 : 2 - e;
+    up = bad ? nan : ldexpf(1.f, k);
+    more = ldexpf(1.f, 2 - e - k);
+    scale = bad ? nan : ldexpf(rstd, e - 2);
 }
 
 struct NormFwd {
@@ -152,9 +154,13 @@ __global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T
         const float rstd = 1.f / sqrtf(ss * inv + a.eps);
         float up = rstd;
         if (scaled) {
-            float down;
-            const bool bad = norm_scale(top, up, down);
-            if (j == 0) a.scale[r] = bad ? f32_of_bits(0x7FC00000u) : rstd * down;
+            float more, scale;
+            norm_scale(top, rstd, up, more, scale);
+            if (j == 0) a.scale[r] = scale;
+            if (more != 1.f) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] *= more;
+            }
         }
         if (a.rstd && j == 0) a.rstd[r] = rstd;
 #pragma unroll
@@ -189,16 +195,16 @@ __global__ __launch_bounds__(256) void rmsnorm_fwd_kernel(NormFwd a) {
     }
     const float rstd = 1.f / sqrtf(block_sum(ss, part) / (float)a.cols + a.eps);
     if (a.rstd && t == 0) a.rstd[r] = rstd;
-    float up = rstd;
+    float up = rstd, more = 1.f;
     if (a.scale) {
         top = block_max_u32(top, partu);
-        float down;
-        const bool bad = norm_scale(top, up, down);
-        if (t == 0) a.scale[r] = bad ? f32_of_bits(0x7FC00000u) : rstd * down;
+        float scale;
+        norm_scale(top, rstd, up, more, scale);
+        if (t == 0) a.scale[r] = scale;
     }
     for (int64_t j = t; j < a.cols; j += 256) {
         const float v = load_value(h, hrow + j, kh, fh) * load_value(a.w, j, a.kw, a.fw);
-        store_value(a.y, r * a.ldy + j, a.ky, a.fy, v * up);
+        store_value(a.y, r * a.ldy + j, a.ky, a.fy, v * more * up);
     }
 }
 
