@@ -233,10 +233,12 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(LogprobFwd a) {
     }
 
     auto element = [&](const uint32_t* w, int e) -> uint32_t { return B == 4 ? w[e] : (w[e * B / 4] >> (8 * B * (e % (4 / B)))) & (B == 1 ? 0xFFu : 0xFFFFu); };
-    // 16-bit posits: zero as 2^-60 or less (es is 1 or 2), which no sum here sees; NaR is looked for by itself
+    // 16-bit posits: NaR, which is looked for by itself, comes out as zero here
     auto value = [&](uint32_t x) -> float {
+        if (K != KIND_POSIT_U16) return value_of<K>(x, a.f);
         uint32_t y;
-        return K == KIND_POSIT_U16 ? posit_value_regular(x, a.f, y) : value_of<K>(x, a.f);
+        const float v = posit_value_regular(x, a.f, y);
+        return y == 0u ? 0.f : v;
     };
     auto order = [&](uint32_t x) -> uint32_t { return POSIT ? lp_order_posit(x, a.f) : lp_order(value(x)); };
     // the largest of a vector, as its order; for 16-bit posits the smallest too (NaR is the smallest of all)
