@@ -119,6 +119,8 @@ def _work(nbytes, device, workspace):
         if nbytes == 0:
             return None, 0, None
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+        raise PositError("workspace must be a dense device tensor")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
