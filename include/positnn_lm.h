@@ -4,7 +4,9 @@
  *
  * The conventions of positnn.h hold: device pointers owned by the caller, calls asynchronous on `stream`, no
  * device memory allocated, freed or kept, a pnn_status from every function, nothing launched where the
- * arguments are refused, zero-sized problems PNN_OK.  In addition:
+ * arguments are refused, zero-sized problems PNN_OK with nothing touched.  That is a problem without rows, columns or
+ * vocabulary, without sequences, heads or elements of a head, and attention without queries (backward: without
+ * queries and keys): sums over nothing (dw of no rows, a row's statistics where it has no columns) are the caller's to fill in.  In addition:
  *  - An element format is a posit of at most 16 bits, PNN_BF16 or PNN_F32 (PNN_EUNSUPPORTED for posit<32,2> and
  *    PNN_F64, PNN_EINVAL for an unknown code).  Posit tensors hold patterns.  NaR reads as NaN, and a NaN or an
  *    infinity that is stored in a posit format becomes NaR; a nonzero finite value never becomes zero in one.

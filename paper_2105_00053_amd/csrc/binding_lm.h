@@ -78,7 +78,7 @@ PyObject* rmsnorm_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const bool scaled = a.i[5] != 0;
         float eps;
         const at::Tensor *x = lm_tensor(a.o[1], fx, 2), *w, *res = nullptr;
-        if (!x || !lm_format(fy) || !lm_real(a.o[0], &eps) || !lm_weight(a.o[2], fw, x->size(1), &w)) return none();
+        if (!x || x->size(1) == 0 || !lm_format(fy) || !lm_real(a.o[0], &eps) || !lm_weight(a.o[2], fw, x->size(1), &w)) return none();
         if (a.o[3] != Py_None && (!(res = lm_tensor(a.o[3], fres, 2)) || res->sizes() != x->sizes())) return none();
         const int64_t rows = x->size(0), cols = x->size(1);
         at::Tensor y, scale, out, rstd;
@@ -178,6 +178,7 @@ PyObject* attention_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const at::Tensor* t[4];
         pnn_attention_desc d;
         if (!lm_format(fout) || (fcopy != -1 && !lm_format(fcopy)) || !lm_attention(fq, fkv, a.o[1], a.o[2], a.o[3], a.o[4], a.o[0], a.i[4], a.i[5], t, &d)) return none();
+        if (d.D == 0) return none();
         at::Tensor o, lse, copy, ws;
         int status;
         {

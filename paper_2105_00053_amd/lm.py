@@ -141,6 +141,8 @@ def posit_rmsnorm_fwd(x, w, fx, fw, fy, eps=1e-6, res=None, fres=None, scaled=Fa
             return _returned(r)
     xp, ldx = _matrix(x, fx, "x")
     rows, cols = x.shape
+    if cols == 0 and rows > 0:
+        raise PositError("x has no columns")
     res_out, rp, ldr, op, ldo = None, None, 0, None, 0
     if res is not None:
         rp, ldr = _matrix(res, fres, "res", x.shape)
@@ -224,6 +226,8 @@ def posit_attention_fwd(q, k, v, fq, fkv, fout, scale=None, window=0, sinks=0, l
             return _returned(r)
     desc, lp = _attention(q, k, v, fq, fkv, scale, window, sinks, lens)
     b, lq, hq, d = q.shape
+    if d == 0 and b * lq * hq > 0:
+        raise PositError("heads have no elements")
     o = torch.empty((b, lq, hq, d), dtype=_dtype(fout), device=q.device)
     lse = torch.empty((b, hq, lq), dtype=torch.float32, device=q.device)
     copy = None if fcopy is None else torch.empty((b, lq, hq, d), dtype=_dtype(_code(fcopy)), device=q.device)
