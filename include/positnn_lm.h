@@ -14,6 +14,9 @@
  *    of them with 8 significant bits are exact there), sums and softmax statistics are kept in binary32, and each
  *    output is rounded once, to its format.  Results do not depend on other work on the device: no sum is taken in
  *    an order that varies from call to call.
+ *  - Sizes: fewer than 2^31 rows and columns, a vocabulary below 2^31; in attention B < 16384, HQ < 65536, D <= 128, LQ * HQ / HKV and LK at
+ *    most 2^31 - 128, and no more rows and keys than the workgroups of a launch (else PNN_EUNSUPPORTED).  Squares and exponents have binary32's range: a row whose
+ *    sum of squares passes it has rstd 0, a logit whose product with the inverse temperature does counts as infinite.
  *  - ld* are row pitches in elements, at least the row's length (else PNN_EINVAL).  Any alignment that the element
  *    type has is accepted.  A workspace is 16-byte aligned (else PNN_EINVAL) and at least as large as the matching
  *    query says (else PNN_EWORKSPACE); its contents on entry do not matter and are not preserved.
@@ -85,7 +88,9 @@ int posit_attention_fwd(void* stream, int fq, int fkv, int fout, const pnn_atten
 
 /* Gradients for d_o (fd, one of the formats of q; strides of q):  P = exp(s - lse),  dV = P^T dO,  dS = P * (dO V^T - rowsum(dO * o)),
  * dQ = scale * dS K,  dK = scale * dS^T Q;  dK and dV are summed over the query heads that share them.  o (fo, dense) and lse
- * are outputs of the forward call.  dq is dense like o, dk and dv dense [b][j][h'][d], all in fout; keys that nothing sees get zeros. */
+ * are outputs of the forward call; D = rowsum(dO * o) is as exact as fo, so where fout of that call is narrow pass its o_copy.  dq is dense like o, dk and
+ * dv dense [b][j][h'][d], all in fout; keys that nothing sees get zeros.  P and dS go into the products behind them rounded to 16 bits, or to 8 where fout is
+ * PNN_BF16, which keeps no more: PNN_F32 gradients are the more exact ones. */
 int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo, int fout, const pnn_attention_desc* desc, const void* d_o,
                         const void* q, const void* k, const void* v, const int32_t* lens, const void* o, const float* lse,
                         void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes);

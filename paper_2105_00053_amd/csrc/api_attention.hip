@@ -39,7 +39,10 @@ struct Plan {
 };
 
 // Few queries on many keys go to the token kernel: it decodes a cache where it reads it and splits its length over workgroups; the
-// prompt kernel reads a packed copy and has a workgroup to 128 rows.
+// prompt kernel reads a packed copy and has a workgroup to 128 rows.  The token kernel reads and decodes the cache once for each 16 rows.  us, token and prompt kernel, heads of
+// 128: 16 rows a group, 8 groups of 8-bit posits, 128 keys 9 and 16, 4096 keys 17 and 102; 384 groups, 12 and 33, 117 and 530.  64 rows, 8 groups, 512 keys 16 and 25, 4096 25
+// and 107; 384 groups 53 and 72, 303 and 540; bfloat16, 384 groups, 65 and 60, 460 and 462: there the two meet.  Beyond 64 rows the better one depends on the number of groups, too: 96
+// rows of bfloat16, 4096 keys, 384 groups 665 and 466, but 8 groups 34 and 101.
 struct TokenPlan {
     bool use;
     int blocks, parts, tiles;  // row blocks of 16, parts of the keys, tiles of 32 keys in a part
@@ -226,7 +229,8 @@ extern "C" int posit_attention_fwd(void* stream, int fq, int fkv, int fout, cons
     a.nbh = (int)p.nbh;
     a.flags = flags; a.marks = marks;
     // The probabilities to 16 bits where an output's format keeps more than 8.  In the copy that the backward pass reads, what the rounding to 8 takes from
-    // a row is common to all its gradients of scores (error of dq 2.6e-3 rather than 2.4e-3, 1.7e-3 of it its own rounding to bfloat16).
+    // a row is common to all its gradients of scores (error of dq 2.6e-3 rather than 2.4e-3, 1.7e-3 of it its own rounding to bfloat16).  With bfloat16 outputs alone, 8
+    // bits: 4 sequences of 2048, 16 heads on 4 of 64, 64 us rather than 82, error of o 2.1e-3 rather than 1.6e-3.
     if (fout != PNN_BF16 || (o_copy && fcopy != PNN_BF16)) launch_fwd<true>(st, p, a);
     else launch_fwd<false>(st, p, a);
     return hip_status(hipGetLastError());
@@ -275,6 +279,7 @@ extern "C" int posit_attention_bwd(void* stream, int fd, int fq, int fkv, int fo
     a.kout = kind_of(fout); a.fout = elem_fmt(fout); a.nbh = (int)p.nbh;
     a.parts = dkv_parts(p); a.part = (float*)(flags + p.nbh * p.s.qblocks);
     a.flags = flags; a.marks = marks;
+    // probabilities and score gradients to 8 bits for bfloat16 gradients, else to 16 (both sides: attn_bwd.h)
     if (fout == PNN_BF16) launch_bwd<false>(st, p, a);
     else launch_bwd<true>(st, p, a);
     return hip_status(hipGetLastError());

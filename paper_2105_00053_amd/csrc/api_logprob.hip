@@ -9,8 +9,8 @@
 // bounds the k-th largest of all from below, and few logits are above it (about k + k^2 / 512 for random ones).  Those are collected and ranked by
 // counting.  Where more are above it than the list holds, k rounds of a maximum take its place.
 // What bounds it: the launch where rows are few (one of 100003 16-bit posits, 20 alternatives: 9 us and 7 for the join of 49 parts), an atomic addition in
-// LDS a logit of 8 bits (2048 rows of 50021, 8 alternatives: 42 us for 102 MB, 2.5 TB/s), the vector unit's decoding and exponentials for 16 bits (4096 rows of 32000:
-// 97 to 104 us for 262 MB, 2.6 TB/s).
+// LDS a logit of 8 bits (2048 rows of 50021, 8 alternatives: 39 to 41 us for 102 MB, 2.5 TB/s; LDS 27 % of the cycles, nearly half of it conflicts, waves waiting 43 %), the
+// vector unit's decoding and exponentials for 16 bits (4096 rows of 32000: 95 to 107 us for 262 MB, 2.6 TB/s; vector unit 85 %).  bfloat16 65 to 71 us, binary32 104 to 110 and 8 for the join.
 #include "lm_codec.h"
 
 namespace pnn {
@@ -477,8 +477,8 @@ struct LogprobBwd {
     int parts;
 };
 
-// Bound by memory: a part of a row to a workgroup, vectors of 8 to a thread, the next one in flight.  4096 rows of 32000 16-bit posits to
-// bfloat16: 117 to 130 us for 524 MB, 4.3 TB/s.
+// A part of a row to a workgroup, vectors of 8 to a thread, the next one in flight.  Bound by the vector unit for 16-bit posits (93 % of the cycles: decoding, an
+// exponential, rounding), with memory not far: 4096 rows of 32000 to bfloat16 117 to 131 us for 524 MB, 4.3 TB/s; from bfloat16 80 to 94, from binary32 139 to 142 for 786 MB.
 template <int K>
 __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwd a) {
     const int t = threadIdx.x;
@@ -520,7 +520,8 @@ __global__ __launch_bounds__(256) void logprob_bwd_kernel(LogprobBwd a) {
 inline int64_t logprob_span(int fz, int64_t rows, int64_t vocab) {
     int64_t span = 16 * 2048 * 2 / (int64_t)element_bytes(fz);
     // A row that fits one workgroup's registers stays whole: the second kernel costs more than the parts save (32 rows, five alternatives, us: 5003 logits in
-    // binary32 8.0 and 11.9, 16384 in 16-bit posits 10.9 and 12.8, 50021 in 8-bit ones 14.0 and 14.6; 32000 in 16-bit ones 14.4 and 13.5).
+    // binary32 8.0 and 11.9, 16384 in 16-bit posits 10.9 and 12.8, 50021 in 8-bit ones 14.0 and 14.6; only 32000 in 16-bit ones, 14.4 and 13.5, would gain from
+    // parts, by less than a rule with a second border is worth).
     if (vocab <= span) return span;
     while (span > 2048 && rows * ((vocab + span - 1) / span) < 512) span /= 2;
     return span;

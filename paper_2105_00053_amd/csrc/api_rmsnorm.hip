@@ -1,8 +1,10 @@
 // posit_rmsnorm_fwd / posit_rmsnorm_bwd / posit_scale_rows: the RMS norm of a residual stream, its gradient, and rows times scales.
 //
-// y = h w / sqrt(mean h^2 + eps), h = x + r.  Bound by memory where rows are many, by the launch where they are few.  16384 rows of 4096, 8-bit
-// posits on a stream of 16-bit ones to bfloat16: forward 122 to 141 us for 470 MB (3.8 TB/s; a large copy reaches 5.2), backward 110 to 114 for
-// 537 MB.  4099 rows of 5119, odd pitches, bfloat16 stream to 8-bit posits with scales: 51; four rows of 2048: 5.
+// y = h w / sqrt(mean h^2 + eps), h = x + r.  Where rows are many the forward kernel is bound by the vector unit (decoding and rounding posits: busy 87 % of the
+// cycles), the backward one by memory (vector unit 56 %); where they are few, by the launch.  16384 rows of 4096, 8-bit posits on a stream of 16-bit ones to
+// bfloat16: forward 115 us in a row of calls (120 to 141 traced alone) for 470 MB, 4.1 TB/s where a large copy reaches 5.2; backward 110 to 114 for 537 MB, 4.9 TB/s.
+// 4099 rows of 5119, odd pitches, bfloat16 stream to 8-bit posits with scales: 46 (traced 52; waves wait 62 % of their time for loads and stores of odd rows, even ones of 5120
+// take 40); four rows of 2048: 5.
 #include "lm_codec.h"
 
 namespace pnn {
@@ -171,7 +173,8 @@ __global__ __launch_bounds__(1024) void rmsnorm_fwd_rows_kernel(NormFwd a, int T
     }
 }
 
-// Longer rows, one to a workgroup: the sum of squares, then the outputs from the stream read again.
+// Longer rows, one to a workgroup: the sum of squares, then the outputs from the stream read again.  Element by element, kinds looked up for each: simple
+// rather than fast.  4096 rows of 12288, 8-bit posits on a stream of 16-bit ones: 456 us for 352 MB; rmsnorm_bwd_kernel 426, rmsnorm_dw_kernel 2.7 ms (48 workgroups).
 __global__ __launch_bounds__(256) void rmsnorm_fwd_kernel(NormFwd a) {
     __shared__ float part[4];
     __shared__ uint32_t partu[4];
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_kernel(NormBwd a) {
     store_value(a.dw, j, a.kdw, a.fdw, s);
 }
 
-// 8 elements to a thread; 4099 x 5119 in 8-bit posits 21 us (both sides unaligned), four rows of 2048 2.
+// 8 elements to a thread; 4099 x 5119 in 8-bit posits to binary32 21 us, 5 TB/s (both sides unaligned), four rows of 2048 2.
 __global__ __launch_bounds__(256) void scale_rows_kernel(const void* x, int64_t ldx, int kx, ElemFmt fx, const float* scale, void* y, int64_t ldy, int ky, ElemFmt fy,
                                                          int64_t rows, int64_t cols, uint32_t vectors) {
     const uint32_t id = blockIdx.x * 256u + threadIdx.x, r = id / vectors;
@@ -390,8 +393,9 @@ inline NormPlan norm_plan(int64_t rows, int64_t cols, int waves) {
     return p;
 }
 
-// What the kernels' registers leave room for (forward up to 72 of 512, backward up to 128).  us with 32, 28 and 16 waves to a compute unit: forward, 4099 rows of
-// 5119, 51, 45 and 66; 16384 of 4096, 101, 97 and 107; backward 75, 70 and 64; 94, 92 and 87; 2000 rows of 3000, 31, 27 and 22.
+// What the kernels' registers leave room for (forward up to 72 of 512, backward up to 128).  us in a row of calls with 32, 28 and 16 waves to a compute unit: forward,
+// bfloat16 stream to 8-bit posits with scales, 4099 rows of 5119, 52, 46 and 67; 16384 of 4096, 101, 98 and 108; 16-bit posit stream to bfloat16, 60, 55 and 76; 116, 115 and 121;
+// backward (with dw) of the latter, 74, 69 and 63; 93, 90 and 87; 2000 rows of 3000, 31, 27 and 22.
 constexpr int NORM_FWD_WAVES = 28, NORM_BWD_WAVES = 16;
 
 template <int KX>

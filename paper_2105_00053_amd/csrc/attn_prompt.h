@@ -4,10 +4,10 @@
 // tiles of the sinks, then those of the window.  Per tile and wave, S^T = K Q^T (A: keys, B: the wave's queries, which stay in registers), so a lane
 // holds 32 scores of ONE query: maximum and sum need no exchange but one between the lane's halves.  O^T += V^T P^T takes the probabilities as they
 // are.  Tiles of keys and values come through LDS, two buffers, copied straight from memory while the tile before is worked on.
-// What bounds it: a wave's 32 rows take an operand of 1 KB from LDS for each matrix instruction, which at the full matrix rate is all that LDS gives, and
-// the softmax takes the vector unit about as long as the products take the matrix unit.  2 sequences of 4001, 16 heads on 4 of 128, window 1024, to 8-bit
-// posits (probabilities in two parts): 127 to 132 us, 0.69 PFLOP/s of matrix instructions; 4 of 2048, heads of 64, causal, to bfloat16: 54, 0.64;
-// with a copy in binary32, so in two parts, 68.
+// What bounds it: no unit by itself (matrix 29 to 33 % of the cycles, vector 47 to 64, LDS 11 to 14), but each wave's chain from scores over maxima and
+// exponentials to the second product, with 1.5 (heads of 128) to 2.8 waves on a SIMD to cover it.  2 sequences of 4001, 16 heads on 4 of 128, window 1024, to 8-bit
+// posits (probabilities in two parts): 127 to 134 us, 0.69 PFLOP/s of matrix instructions; 4 of 2048, heads of 64, causal, to bfloat16: 52, 0.66;
+// with a copy in binary32, so in two parts, 69.
 // The running maximum is a reference: results are rescaled only when a row's maximum rises by more than 2^8 above it.
 #pragma once
 

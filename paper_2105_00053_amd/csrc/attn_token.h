@@ -6,8 +6,9 @@
 // where it is used.  8-bit posits go through a table in LDS that every bank has a copy of (32 KB; look-ups without conflicts): two vector
 // operations and a half an element, where the field decoder takes 12.
 //
-// 48 sequences of up to 8192 keys, window 4096, 8 heads of 128 for 32 of queries, 8-bit posits: 96 to 101 us for 335 MB, 3.4 TB/s (look-ups and the
-// vector unit); 16 of 4096 in bfloat16 52, 5.2 TB/s; 16-bit posits by the field decoder 2.3 TB/s.  One sequence of 8192: 21, 3 of 300: 8.
+// 48 sequences of up to 8192 keys, window 4096, 8 heads of 128 for 32 of queries, 8-bit posits: 97 to 101 us for 335 MB, 3.4 TB/s (vector unit 44 % of the cycles, LDS 21,
+// 1.5 waves on a SIMD: latencies of loads and look-ups); 16 of 4096 in bfloat16 48, 5.6 TB/s; in 12-bit posits by the field decoder 120, 2.2 TB/s (vector unit 72 %).  One
+// sequence of 8192: 21, 3 of 300: 8.
 //
 // v_mfma_f32_16x16x32_bf16 (a group of heads rarely has more than 16; on the 32 x 32 form results and q took twice the registers): lane l
 // holds, for A, row l % 16 and the 8 reduction indices from 8 (l / 16); for B, column l % 16 and the same; result register r is row 4 (l / 16) + r,
