@@ -73,9 +73,10 @@ def test_a_diverged_step_takes_about_as_long(pass_, window, sinks):
     """With a NaR in every key's value (every row's error): a wave reads what is noted of a block, a load for each 64 blocks, and walks 32 rows of the blocks at
     its edges, some hundred loads in series of a microsecond at most; the kernel for few queries reads the values a second time."""
     b, l, hq, hkv, d = (64, 8192, 8, 1, 64) if pass_ == "token" else (1, 8192, 4, 1, 64)
-    rng = np.random.default_rng(3)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
     lq = 1 if pass_ == "token" else l
-    q, k, v, do = (to_format(normal(rng, s), "p8_1") for s in ((b, lq, hq, d), (b, l, hkv, d), (b, l, hkv, d), (b, lq, hq, d)))
+    q, k, v, do = (pn.posit_round(torch.randn(s, generator=g, device="cuda"), "p8_1") for s in ((b, lq, hq, d), (b, l, hkv, d), (b, l, hkv, d), (b, lq, hq, d)))
     how = {"window": window, "sinks": sinks}
     o, lse, copy = pn.posit_attention_fwd(q, k, v, "p8_1", "p8_1", "bf16", fcopy="f32", **how)
 
