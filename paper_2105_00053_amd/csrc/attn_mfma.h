@@ -23,6 +23,8 @@ typedef __bf16 at_v8b __attribute__((ext_vector_type(8)));
 typedef uint32_t at_v4u __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ at_v16f at_mfma(at_v8b a, at_v8b b, at_v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+typedef float at_v4f __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ at_v4f at_mfma16(at_v8b a, at_v8b b, at_v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ at_v8b at_frag(const uint4& v) { return __builtin_bit_cast(at_v8b, v); }
 __device__ __forceinline__ at_v16f at_zero() {
     at_v16f z;
@@ -71,6 +73,9 @@ __device__ __forceinline__ int at_snake(int i, int n, int nbh) {
 // What a block of 32 rows holds that is not finite: for each row, and last for all of them together, one bit an element of a head in three
 // masks of 128 (+infinity, -infinity, NaN).
 constexpr int AT_MARKS = 33 * 3;
+
+// Of few queries: workgroups that a row block's keys are split over, what the kernel that joins them holds weights of.
+constexpr int AT_MOST_PARTS = 256;
 
 struct AttnPackItem {
     const void* src;

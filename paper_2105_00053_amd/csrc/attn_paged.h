@@ -1,0 +1,482 @@
+// Attention of a few new tokens on a cache in pages.
+//
+// A workgroup takes 16 rows (positions and heads of a group) of a sequence and a part of the keys that they see; its four waves take tiles of 32 keys in turn, as the kernel of
+// attn_token.h does, whose matrix instructions and orders these are: S^T = K Q^T, then O^T += V^T P^T with the probabilities as they come out of the first product.
+// What differs is where elements come from.  The order of a head's elements in the first product is free, so a lane takes a run of a key's elements (8 for each block of 32), and a
+// page holds four tokens' values side by side, so that a lane's eight values of a block of elements are two runs.  Page numbers are looked up one tile ahead of the loads that need them.
+// 4-bit floats become bfloat16 two at a time with their block's power, in one instruction; 8-bit posits through a table in LDS that every bank has a copy of.
+#pragma once
+
+#include "attn_prompt.h"
+#include "cache_common.h"
+
+namespace pnn {
+
+struct AttnPaged {
+    CacheShape s;
+    AttnShape n;          // window, sinks, G, D, scale, LK: the longest
+    const void* q;
+    const char *k, *v;
+    int64_t ql, qh;
+    int kq, most;
+    ElemFmt fq, fc;
+    void* o;
+    float* lse;
+    int ko;
+    ElemFmt fo;
+    int blocks;           // row blocks of 16
+    int tiles, parts;     // of a part; workgroups that a row block's keys are split over
+    float* part;          // [row block][part][m: 16][l: 16][16][D]
+};
+
+// A sequence's rows and keys
+struct PagedRows {
+    int first, count, rows, keys, base;  // rows: those of the heads of a group; base: the first one's position
+    __device__ __forceinline__ PagedRows(const AttnPaged& a, int b) {
+        first = cache_first(a.s, b);
+        const int end = a.s.starts ? cache_first(a.s, b + 1) : b + 1;
+        count = end > first ? end - first : 0;
+        const int n = a.s.lens[b];
+        keys = n < 0 ? 0 : (n > a.n.LK ? a.n.LK : n);
+        base = keys - count;
+        rows = (count < a.most ? count : a.most) * a.n.G;
+    }
+};
+
+// A tile's keys and values as they lie in memory
+template <int KC, int KS, int NV>
+struct PagedRaw {
+    static constexpr int KW = KC == CACHE_F4 ? 1 : (KC == CACHE_U8 ? 2 : 4);  // words of eight elements
+    uint32_t k[2][KS * KW], v[2][4 * KW];
+    uint32_t kp[2][KC == CACHE_F4 ? KS : 1], vp[KC == CACHE_F4 ? 2 : 1];  // powers
+    bool bad[2];  // the halves' pages are none
+};
+
+template <int KC, int DB>
+__global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kernel(AttnPaged a) {
+    constexpr int KS = DB, NV = DB <= 2 ? 4 : 8;
+    typedef PagedRaw<KC, KS, NV> R;
+    __shared__ uint32_t smem[8192];  // the table, then what the waves join through
+    __shared__ float wm[4][16], wl[4][16];
+    const CacheShape& s = a.s;
+    const AttnShape& n = a.n;
+    const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), quarter = lane >> 4, col = lane & 15;
+    const int hk = blockIdx.y, b = blockIdx.z;
+    const int rb = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - rb * a.parts;
+    const PagedRows x(a, b);
+    if (rb * 16 >= x.rows) return;
+    const int row = rb * 16 + col, last = rb * 16 + 15 < x.rows ? rb * 16 + 15 : x.rows - 1;
+    const int i = row / n.G, h = hk * n.G + (row - i * n.G);
+    const bool live = row < x.rows;
+    const int p = live ? x.base + i : -1, low = n.window ? p - n.window : -1;
+    const int p0 = x.base + rb * 16 / n.G, p1 = x.base + last / n.G;
+    const int low1 = n.window ? p1 - n.window : -1;
+    const AttnTiles tiles = at_tiles<32>(n, p0, p1);
+    const int begin = part * a.tiles, end = begin + a.tiles < tiles.count ? begin + a.tiles : tiles.count;
+    if (a.parts > 1 && part > 0 && begin >= tiles.count) return;
+    const int keys = x.keys, D = n.D;
+
+    auto key_of = [&](int i) { return 16 * (i >> 2) + 4 * quarter + (i & 3); };  // the lane's i-th key of a tile, as scores and as values
+    // the pages of a tile's halves; the last key's in place of those behind it
+    auto page_of = [&](int m, int half) -> int64_t {
+        const int key = tiles.at(m) * 32 + 16 * half;
+        return cache_page(s, b, (key < keys ? key : keys - 1) >> s.shift, hk);
+    };
+    auto load = [&](int m, const int64_t (&pages)[2], R& r) {
+        const int key0 = tiles.at(m) * 32;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            r.bad[y] = pages[y] < 0;
+            const int64_t page = pages[y] < 0 ? 0 : pages[y];
+            const int at0 = (key0 + 16 * y) & (s.page - 1);
+            const char* const kp = a.k + page;
+            const char* const vp = a.v + page;
+            // of a key, the lane's run of 8 KS elements
+            const int at = at0 + col;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const int unit = KS * quarter + ks, el = cache_unit(s, false, at, 8 * unit < D ? unit : 0);
+                __builtin_memcpy(&r.k[y][ks * R::KW], kp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 4 * R::KW);
+                if (KC == CACHE_F4) r.kp[y][ks] = ((const uint8_t*)kp)[cache_power(s, false, at, 8 * unit < D ? unit >> 2 : 0)];
+            }
+            // of four tokens' values, the lane's block of eight elements (a half of it where NV is 4)
+            const int unit = NV * col / 8 < D / 8 ? NV * col / 8 : 0, el = cache_unit(s, true, at0 + 4 * quarter, unit);
+            __builtin_memcpy(r.v[y], vp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 16 * R::KW);
+            if (KC == CACHE_F4) __builtin_memcpy(&r.vp[y], vp + cache_power(s, true, at0 + 4 * quarter, unit >> 2), 4);
+        }
+    };
+    R raw;
+    int64_t pages[2] = {-1, -1};
+    if (begin + w < end) {
+        pages[0] = page_of(begin + w, 0);
+        pages[1] = page_of(begin + w, 1);
+        load(begin + w, pages, raw);
+        if (begin + w + 4 < end) {
+            pages[0] = page_of(begin + w + 4, 0);
+            pages[1] = page_of(begin + w + 4, 1);
+        }
+    }
+
+    if (KC == CACHE_U8) {
+        // low half: the value in bfloat16; high half: the same with zero for NaR (see AttnMarks)
+        const uint32_t bits = bits_of_f32(posit_value(t, a.fc)) >> 16;
+        const uint32_t e = bits | ((bits & 0x7F80u) == 0x7F80u ? 0u : bits << 16);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) ((uint4*)smem)[t * 8 + c] = make_uint4(e, e, e, e);
+        __syncthreads();
+    }
+    const uint32_t* const tab = smem + (lane & 31);
+
+    float c = n.scale * 1.4426950408889634f;
+    at_v8b q[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int d = 8 * (KS * quarter + ks);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (live && d < D) u = at_load8(a.q, (int64_t)(x.first + i) * a.ql + h * a.qh + d, 8, a.kq, a.fq);
+        q[ks] = at_scaled(u, c);
+    }
+    c = at_scale(c);
+
+    // eight elements of a key as bfloat16
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    auto four = [&](uint32_t word, float scale, uint32_t (&o)[4]) {
+        o[0] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+        o[1] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+        o[2] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+        o[3] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
+    };
+    auto entry = [&](uint32_t word, int i) -> uint32_t { return tab[((word >> (8 * i)) & 0xFFu) * 32]; };
+    auto key_words = [&](const uint32_t* e, uint32_t power) -> uint4 {
+        if constexpr (KC == CACHE_F4) {
+            uint32_t o[4];
+            four(e[0], f4_scale(power), o);
+            const uint32_t nan = power == 255u ? 0x7FC07FC0u : 0u;
+            return make_uint4(o[0] | nan, o[1] | nan, o[2] | nan, o[3] | nan);
+        } else if constexpr (KC == CACHE_U8) {
+            auto two = [&](uint32_t word, int i) { return __builtin_amdgcn_perm(entry(word, i + 1), entry(word, i), 0x05040100u); };
+            return make_uint4(two(e[0], 0), two(e[0], 2), two(e[1], 0), two(e[1], 2));
+        } else {
+            return make_uint4(e[0], e[1], e[2], e[3]);
+        }
+    };
+
+    const float inf = f32_of_bits(0x7F800000u), nan = f32_of_bits(0x7FC00000u);
+    float m = -inf, l = 0.f;
+    at_v4f o[NV];
+#pragma unroll
+    for (int y = 0; y < NV; ++y) o[y] = at_v4f{0.f, 0.f, 0.f, 0.f};
+    uint32_t flagged = 0;
+    for (int tile = begin + w; tile < end; tile += 4) {
+        const R cur = raw;
+        if (tile + 4 < end) {
+            load(tile + 4, pages, raw);
+            if (tile + 8 < end) {
+                pages[0] = page_of(tile + 8, 0);
+                pages[1] = page_of(tile + 8, 1);
+            }
+        }
+        const int key0 = tiles.at(tile) * 32;
+        float sc[8];  // of keys key_of(0 .. 7)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            at_v4f acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                uint4 u = key_words(&cur.k[y][ks * R::KW], KC == CACHE_F4 ? cur.kp[y][ks] : 0u);
+                if (D < 32 * DB) u = 8 * (KS * quarter + ks) < D ? u : make_uint4(0, 0, 0, 0);
+                acc = at_mfma16(at_frag(u), q[ks], acc);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[4 * y + r] = cur.bad[y] ? nan : acc[r];
+        }
+        if (!(key0 + 31 <= p0 && (key0 > low1 || key0 + 31 < n.sinks))) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) sc[r] = at_sees(n, p, low, key0 + key_of(r)) ? sc[r] : -inf;
+        }
+        float mx = sc[0];
+#pragma unroll
+        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, sc[r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = at_max_halves(mx) * c;
+        if (__any(mx > m + 8.f)) {
+            const float m1 = fmaxf(m, mx), f = m1 == -inf ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+            m = m1;
+            l *= f;
+#pragma unroll
+            for (int y = 0; y < NV; ++y) o[y] *= f;
+        }
+        const float mr = m == -inf ? 0.f : m;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -mr));
+            l += sc[r];
+        }
+        at_v8b ph, pl;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            ph[r] = (__bf16)sc[r];
+            pl[r] = (__bf16)(sc[r] - (float)ph[r]);
+        }
+
+        // what lies behind the last key is anything: zeros
+        uint32_t v[2][4 * R::KW], vp[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int e = 0; e < 4 * R::KW; ++e) v[y][e] = cur.v[y][e];
+            if (KC == CACHE_F4) vp[y] = cur.vp[y];
+        }
+        if (key0 + 31 >= keys) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = key0 + key_of(4 * y + e) < keys;
+#pragma unroll
+                    for (int z = 0; z < R::KW; ++z) v[y][e * R::KW + z] = in ? v[y][e * R::KW + z] : 0u;
+                    if (KC == CACHE_F4) vp[y] = in ? vp[y] : (vp[y] & ~(0xFFu << (8 * e))) | 127u << (8 * e);
+                }
+        }
+        // NaR, NaN and infinities: zeros, and looked up at the end
+        uint32_t odd = 0;
+        if (KC == CACHE_F4) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y) odd |= (~vp[y] - 0x01010101u) & vp[y] & 0x80808080u;
+        } else if (KC == CACHE_U8) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t z = v[y][e] ^ 0x80808080u;
+                    odd |= (z - 0x01010101u) & ~z & 0x80808080u;
+                }
+        } else {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) odd |= at_odd(v[y][e]) ? 1u : 0u;
+        }
+        flagged |= odd;
+        if (KC != CACHE_U8 && __any(odd != 0)) {
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (KC == CACHE_F4) {
+                        const bool gone = ((vp[y] >> (8 * e)) & 0xFFu) == 255u;
+                        v[y][e] = gone ? 0u : v[y][e];
+                        vp[y] = gone ? vp[y] ^ 128u << (8 * e) : vp[y];
+                    } else {
+#pragma unroll
+                        for (int z = 0; z < 4; ++z) {
+                            uint32_t u = v[y][(4 * e + z) % (4 * R::KW)];
+                            if ((u & 0x7F80u) == 0x7F80u) u &= 0xFFFF0000u;
+                            if ((u & 0x7F800000u) == 0x7F800000u) u &= 0xFFFFu;
+                            v[y][(4 * e + z) % (4 * R::KW)] = u;
+                        }
+                    }
+                }
+        }
+        // the NV elements of each of the lane's eight keys; two keys' to a word
+        const bool high = NV == 4 && (col & 1);
+        if constexpr (KC == CACHE_F4) {
+            uint32_t d[8][4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float scale = f4_scale((vp[e / 4] >> (8 * (e & 3))) & 0xFFu);
+                const uint32_t word = high ? v[e / 4][e & 3] >> 16 : v[e / 4][e & 3];
+                d[e][0] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0));
+                d[e][1] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1));
+                if (NV == 8) {
+                    d[e][2] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2));
+                    d[e][3] = __builtin_bit_cast(uint32_t, (v2b)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3));
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < NV; ++y) {
+                const uint32_t sel = y & 1 ? 0x07060302u : 0x05040100u;
+                const at_v8b f = at_frag(make_uint4(__builtin_amdgcn_perm(d[1][y / 2], d[0][y / 2], sel), __builtin_amdgcn_perm(d[3][y / 2], d[2][y / 2], sel),
+                                                    __builtin_amdgcn_perm(d[5][y / 2], d[4][y / 2], sel), __builtin_amdgcn_perm(d[7][y / 2], d[6][y / 2], sel)));
+                o[y] = at_mfma16(f, ph, o[y]);
+                o[y] = at_mfma16(f, pl, o[y]);
+            }
+        } else {
+            constexpr int KW = R::KW;
+            // words of the lane's NV elements
+            constexpr int W = NV * KW / 8;
+            uint32_t d[8][W];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int z = 0; z < W; ++z) {
+                    const uint32_t first = v[e / 4][(e & 3) * KW + z], second = v[e / 4][(e & 3) * KW + (z + KW / 2) % KW];
+                    d[e][z] = NV == 4 && high ? second : first;
+                }
+#pragma unroll
+            for (int y = 0; y < NV; ++y) {
+                uint32_t u[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (KC == CACHE_U8) u[e] = __builtin_amdgcn_perm(entry(d[2 * e + 1][y / 4 % W], y & 3), entry(d[2 * e][y / 4 % W], y & 3), 0x07060302u);
+                    else u[e] = __builtin_amdgcn_perm(d[2 * e + 1][y / 2 % W], d[2 * e][y / 2 % W], y & 1 ? 0x07060302u : 0x05040100u);
+                }
+                const at_v8b f = at_frag(make_uint4(u[0], u[1], u[2], u[3]));
+                o[y] = at_mfma16(f, ph, o[y]);
+                o[y] = at_mfma16(f, pl, o[y]);
+            }
+        }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (__any(flagged != 0)) {
+        // the wave's tiles once more, an element of a value to a lane
+        AttnMarks<DB> marks = {};
+        for (int tile = begin + w; tile < end; tile += 4) {
+            const int64_t at[2] = {page_of(tile, 0), page_of(tile, 1)};
+#pragma unroll 4
+            for (int r = 0; r < 32; ++r) {
+                const int key = tiles.at(tile) * 32 + r;
+                const char* const from = a.v + (at[r >> 4] < 0 ? 0 : at[r >> 4]);
+                uint32_t mk[3][4] = {};
+#pragma unroll
+                for (int y = 0; y < (DB + 1) / 2; ++y) {
+                    const int d = 64 * y + lane;
+                    float v = 0.f;
+                    if (d < D && key < keys) {
+                        const int slot = key & (s.page - 1), el = cache_unit(s, true, slot, d >> 3) + (d & 7);
+                        if (KC == CACHE_F4) v = ((const uint8_t*)from)[cache_power(s, true, slot, d >> 5)] == 255u ? nan : 0.f;
+                        else if (KC == CACHE_U8) v = posit_value(((const uint8_t*)from)[el], a.fc);
+                        else v = f32_of_bits((uint32_t)((const uint16_t*)from)[el] << 16);
+                    }
+                    const uint64_t bits[3] = {__ballot(v == inf), __ballot(v == -inf), __ballot(v != v)};
+#pragma unroll
+                    for (int z = 0; z < 3; ++z) {
+                        mk[z][2 * y] = (uint32_t)bits[z];
+                        mk[z][2 * y + 1] = (uint32_t)(bits[z] >> 32);
+                    }
+                }
+                marks.add(mk[0], mk[1], mk[2], at_sees(n, p, low, key));
+            }
+        }
+        // the lane's elements NV (4 quarter + r) + y lie in one word
+        const int word = NV * quarter / 8, from = NV * 4 * quarter & 31;
+        uint32_t mp = 0, mn = 0, mq = 0;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            mp = word == d ? marks.pos[d] : mp;
+            mn = word == d ? marks.neg[d] : mn;
+            mq = word == d ? marks.nan[d] : mq;
+        }
+#pragma unroll
+        for (int y = 0; y < NV; ++y)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[y][r] = at_marked(o[y][r], mp, mn, mq, from + NV * r + y);
+    }
+
+    // join the waves: a common reference, then through LDS, [wave][block][element row][column]
+    if (quarter == 0) {
+        wm[w][col] = m;
+        wl[w][col] = l;
+    }
+    __syncthreads();
+    const float top = fmaxf(fmaxf(wm[0][col], wm[1][col]), fmaxf(wm[2][col], wm[3][col]));
+    const float f = m == -inf ? 1.f : __builtin_amdgcn_exp2f(m - top);
+    float* const red = (float*)smem;
+#pragma unroll
+    for (int y = 0; y < NV; ++y)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float u = o[y][r];
+            red[((w * NV + y) * 16 + 4 * quarter + r) * 16 + col] = u - u == 0.f ? u * f : u;  // an infinity stays one
+        }
+    __syncthreads();
+    // NV neighbouring elements of a row to a thread
+    const int rr = t >> 4, rho = t & 15, gr = rb * 16 + rr, d = NV * rho;
+    if (gr >= x.rows) return;
+    float out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int y = 0; y < NV; ++y)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) out[y] += red[((z * NV + y) * 16 + rho) * 16 + rr];
+    float mm = -inf, sum = 0.f;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) mm = fmaxf(mm, wm[z][rr]);
+#pragma unroll
+    for (int z = 0; z < 4; ++z) sum += wm[z][rr] == -inf ? wl[z][rr] : wl[z][rr] * __builtin_amdgcn_exp2f(wm[z][rr] - mm);
+    if (a.parts > 1 && tiles.count > a.tiles) {
+        float* const at = a.part + ((((int64_t)b * s.HKV + hk) * a.blocks + rb) * a.parts + part) * (16 * (D + 2));
+        if (rho == 0) {
+            at[rr] = mm;
+            at[16 + rr] = sum;
+        }
+#pragma unroll
+        for (int y = 0; y < NV; ++y)
+            if (d + y < D) at[32 + rr * D + d + y] = out[y];
+        return;
+    }
+    const int gi = gr / n.G, gh = hk * n.G + (gr - gi * n.G);
+    const int64_t to = (int64_t)(x.first + gi) * (s.HKV * n.G) + gh;
+    if (a.lse && rho == 0) a.lse[to] = sum == 0.f ? -inf : mm * 0.6931471805599453f + logf(sum);
+    const float up = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) out[y] *= up;
+    at_store8(a.o, to * D + d, D - d < NV ? D - d : NV, a.ko, a.fo, out);
+}
+
+// Parts of a row joined, one row to a workgroup and an element to a thread; rows whose keys are in one part are done.
+__global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
+    __shared__ float weight[AT_MOST_PARTS];
+    __shared__ float half_max[2], half_sum[2];
+    const AttnShape& n = a.n;
+    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x, rr = row & 15, rb = row >> 4, D = n.D;
+    const PagedRows x(a, b);
+    if (row >= x.rows) return;
+    const int i = row / n.G, h = hk * n.G + (row - i * n.G);
+    const int last = rb * 16 + 15 < x.rows ? rb * 16 + 15 : x.rows - 1;
+    const int count = at_tiles<32>(n, x.base + rb * 16 / n.G, x.base + last / n.G).count;
+    if (count <= a.tiles) return;
+    const int parts = (count + a.tiles - 1) / a.tiles;
+    const int64_t step = 16 * (D + 2);
+    const float* const at = a.part + ((((int64_t)b * a.s.HKV + hk) * a.blocks + rb) * a.parts) * step;
+    const float inf = f32_of_bits(0x7F800000u);
+    float mine[AT_MOST_PARTS / 128], sums[AT_MOST_PARTS / 128], m = -inf, l = 0.f;
+#pragma unroll
+    for (int y = 0; y < AT_MOST_PARTS / 128; ++y) {
+        const int p = t + 128 * y;
+        mine[y] = p < parts ? at[p * step + rr] : -inf;
+        sums[y] = p < parts ? at[p * step + 16 + rr] : 0.f;
+        m = fmaxf(m, mine[y]);
+    }
+    m = wave_max(m);
+    if ((t & 63) == 0) half_max[t >> 6] = m;
+    __syncthreads();
+    m = fmaxf(half_max[0], half_max[1]);
+#pragma unroll
+    for (int y = 0; y < AT_MOST_PARTS / 128; ++y) {
+        const float f = mine[y] == -inf ? 1.f : __builtin_amdgcn_exp2f(mine[y] - m);  // a part without keys: zeros, or NaN
+        weight[t + 128 * y] = f;
+        l += sums[y] * f;
+    }
+    l = wave_sum(l);
+    if ((t & 63) == 0) half_sum[t >> 6] = l;
+    __syncthreads();
+    l = half_sum[0] + half_sum[1];
+    const int64_t to = (int64_t)(x.first + i) * (a.s.HKV * n.G) + h;
+    if (a.lse && t == 0) a.lse[to] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
+    if (t >= D) return;
+    const float* const from = at + 32 + rr * D + t;
+    float o = 0.f;
+    for (int p = 0; p < parts; p += 8) {
+        float v[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] = from[(p + y < parts ? p + y : 0) * step];
+#pragma unroll
+        for (int y = 0; y < 8; ++y)
+            if (p + y < parts) o += v[y] - v[y] == 0.f ? v[y] * weight[p + y] : v[y];
+    }
+    o = l == 0.f ? 0.f : o / l;
+    store_value(a.o, to * D + t, a.ko, a.fo, o);
+}
+
+}  // namespace pnn

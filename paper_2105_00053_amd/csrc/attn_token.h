@@ -21,11 +21,7 @@
 
 namespace pnn {
 
-typedef float at_v4f __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ at_v4f at_mfma16(at_v8b a, at_v8b b, at_v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-
 constexpr int AT_TOKEN_ROWS = 16;
-constexpr int AT_MOST_PARTS = 256;  // workgroups to a row block's keys, what the second kernel holds weights of
 
 struct AttnToken {
     AttnShape s;

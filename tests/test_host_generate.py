@@ -1,0 +1,200 @@
+"""The entry points that generate text are declared, exported and refuse what their header says they refuse (nothing is launched)."""
+import ctypes
+import os
+import re
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "positnn_generate.h")
+
+EINVAL, EUNSUPPORTED, EWORKSPACE = 1, 2, 3
+FAKE = ctypes.c_void_p(0x1000)  # never dereferenced
+NULL = ctypes.c_void_p(0)
+
+
+@pytest.fixture(scope="module")
+def L():
+    from paper_2105_00053_amd import build, generate
+    if not os.path.exists(build.LIB):
+        build.build()
+    return generate._load()
+
+
+def test_declared_functions_are_exported(L):
+    src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    names = set(re.findall(r"\b(posit_[a-z0-9_]+)\s*\(", src))
+    assert names == {"posit_qk_norm_rope_fwd", "posit_qk_norm_rope_bwd", "posit_qk_norm_rope_bwd_workspace", "posit_cache_append", "posit_cache_read",
+                     "posit_attention_paged", "posit_attention_paged_workspace", "posit_sample", "posit_sample_workspace"}
+    for n in names:
+        assert hasattr(L, n)
+
+
+def test_the_header_is_c(tmp_path):
+    if shutil.which("gcc") is None:
+        pytest.skip("no C compiler")
+    src = tmp_path / "t.c"
+    src.write_text('#include "positnn_generate.h"\nint main(void) { pnn_heads_desc h; pnn_paged_desc p; h.D = PNN_F4; p.D = PNN_F4; return h.D == p.D ? 0 : 1; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-c", str(src), "-o", str(tmp_path / "t.o")], check=True)
+
+
+def test_the_structures_are_the_headers():
+    """Fields in the header's order: sizes as a C compiler has them."""
+    from paper_2105_00053_amd import HeadsDesc, PagedDesc
+    src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    for name, cls in (("pnn_heads_desc", HeadsDesc), ("pnn_paged_desc", PagedDesc)):
+        body = re.search(r"typedef struct \{([^}]*)\} %s;" % name, src).group(1)
+        fields = [(f.strip(), t) for t, line in re.findall(r"(int64_t|int32_t|float) ([^;]*);", body) for f in line.split(",")]
+        types = {"int64_t": ctypes.c_int64, "int32_t": ctypes.c_int32, "float": ctypes.c_float}
+        assert [(f, types[t]) for f, t in fields] == list(cls._fields_)
+
+
+def heads(**kw):
+    from paper_2105_00053_amd import HeadsDesc
+    return HeadsDesc(**dict(dict(T=4, HQ=4, HKV=2, D=64, R=64, ql=256, qh=64, kl=128, kh=64, gql=256, gqh=64, gkl=128, gkh=64, neighbours=0, eps=1e-6), **kw))
+
+
+def test_heads_refusals(L):
+    def fwd(d, fx=3, fw=1, fy=102, q=FAKE, k=FAKE, wq=FAKE, wk=FAKE, pos=FAKE, freq=FAKE, yq=FAKE, yk=FAKE):
+        return L.posit_qk_norm_rope_fwd(NULL, fx, fw, fy, ctypes.byref(d), q, k, wq, wk, pos, freq, yq, yk, FAKE)
+
+    def bwd(d, fd=3, fx=3, fw=1, fdx=102, fdw=100, g=FAKE, q=FAKE, wq=FAKE, wk=FAKE, rstd=FAKE, freq=FAKE, dq=FAKE, dwq=FAKE, ws=FAKE, n=1 << 40):
+        return L.posit_qk_norm_rope_bwd(NULL, fd, fx, fw, fdx, fdw, ctypes.byref(d), g, FAKE, q, FAKE, wq, wk, rstd, FAKE, freq, dq, FAKE, dwq, FAKE, ws, n)
+
+    assert L.posit_qk_norm_rope_fwd(NULL, 3, 1, 102, None, *[FAKE] * 9) == EINVAL
+    for bad in (dict(T=-1), dict(HQ=-1), dict(HKV=-1), dict(D=-2), dict(R=-2), dict(R=66), dict(R=33), dict(eps=-1.0), dict(eps=float("nan")), dict(ql=-1), dict(kh=-1)):
+        assert fwd(heads(**bad)) == bwd(heads(**bad)) == EINVAL, bad
+    assert bwd(heads(gqh=-1)) == EINVAL
+    for bad in (dict(D=63, R=0), dict(D=258), dict(T=2 ** 31), dict(HQ=65536), dict(HQ=65000, HKV=1000)):
+        assert fwd(heads(**bad)) == bwd(heads(**bad)) == EUNSUPPORTED, bad
+    for f in (2, 101):
+        assert fwd(heads(), fx=f) == fwd(heads(), fw=f) == fwd(heads(), fy=f) == bwd(heads(), fd=f) == bwd(heads(), fdx=f) == bwd(heads(), fdw=f) == EUNSUPPORTED
+    assert fwd(heads(), fx=77) == fwd(heads(), fx=103) == bwd(heads(), fd=77) == EINVAL
+    assert fwd(heads(), q=NULL) == fwd(heads(), k=NULL) == fwd(heads(), yq=NULL) == fwd(heads(), yk=NULL) == fwd(heads(), wq=NULL) == fwd(heads(), wk=NULL) == EINVAL
+    assert fwd(heads(), freq=NULL) == bwd(heads(), freq=NULL) == EINVAL
+    assert bwd(heads(), g=NULL) == bwd(heads(), q=NULL) == bwd(heads(), rstd=NULL) == bwd(heads(), dq=NULL) == bwd(heads(), wq=NULL) == EINVAL
+    assert bwd(heads(), wq=NULL, wk=NULL) == EINVAL  # a weight's gradient without weights
+    assert fwd(heads(T=0), q=NULL) == fwd(heads(HQ=0, HKV=0), q=NULL) == fwd(heads(D=0, R=0), q=NULL) == bwd(heads(T=0), q=NULL) == 0
+    need = L.posit_qk_norm_rope_bwd_workspace(ctypes.byref(heads()))
+    assert need > 0 and L.posit_qk_norm_rope_bwd_workspace(ctypes.byref(heads(T=0))) == 0
+    assert bwd(heads(), n=need - 1) == bwd(heads(), ws=NULL) == EWORKSPACE
+    assert bwd(heads(), ws=ctypes.c_void_p(0x1008)) == EINVAL
+
+
+def paged(**kw):
+    from paper_2105_00053_amd import PagedDesc
+    return PagedDesc(**dict(dict(T=3, B=3, HQ=4, HKV=2, D=64, R=64, page=16, pages=9, columns=4, pitch=4, ql=256, qh=64, kl=128, kh=64, vl=128, vh=64, window=0, sinks=0,
+                                 most=1, longest=64, scale=0.125, eps=1e-6, neighbours=0), **kw))
+
+
+BAD = (dict(T=-1), dict(B=-1), dict(HKV=-1), dict(D=-8), dict(page=0), dict(page=-16), dict(pages=-1), dict(columns=-1), dict(pitch=3))
+TOO_MUCH = (dict(page=8), dict(page=24), dict(page=8192), dict(D=60, R=0), dict(D=136), dict(T=2 ** 31, B=2 ** 31), dict(B=65536, T=65536), dict(HKV=65536, HQ=65536), dict(pages=2 ** 31),
+            dict(columns=2 ** 28, pitch=2 ** 28))
+
+
+def test_append_refusals(L):
+    def call(d, fx=3, fw=1, fq=102, fc=3, q=FAKE, k=FAKE, wq=FAKE, wk=FAKE, starts=NULL, lens=FAKE, table=FAKE, kc=FAKE, yq=FAKE):
+        return L.posit_cache_append(NULL, fx, fw, fq, fc, ctypes.byref(d), q, k, FAKE, wq, wk, FAKE, starts, lens, table, kc, FAKE, yq)
+
+    assert L.posit_cache_append(NULL, 3, 1, 102, 3, None, *[FAKE] * 12) == EINVAL
+    for bad in BAD + (dict(R=-2), dict(R=66), dict(R=31), dict(eps=-1.0), dict(eps=float("nan")), dict(ql=-1), dict(kl=-1), dict(vh=-1)):
+        assert call(paged(**bad)) == EINVAL, bad
+    for bad in TOO_MUCH:
+        assert call(paged(**bad)) == EUNSUPPORTED, bad
+    for f in (1, 2, 5, 8, 100, 101):
+        assert call(paged(), fc=f) == EUNSUPPORTED, f
+    assert call(paged(), fc=77) == call(paged(), fx=103) == call(paged(), fq=103) == EINVAL
+    assert call(paged(), fx=2) == call(paged(), fw=2) == call(paged(), fq=101) == EUNSUPPORTED
+    assert call(paged(T=4)) == EINVAL                       # rows and sequences without starts
+    assert call(paged(), k=NULL) == call(paged(), lens=NULL) == call(paged(), table=NULL) == call(paged(), kc=NULL) == call(paged(), yq=NULL) == EINVAL
+    assert call(paged(), wq=NULL) == call(paged(), wk=NULL) == EINVAL
+    assert call(paged(), kc=ctypes.c_void_p(0x1008)) == EINVAL
+    assert call(paged(T=0, B=0), k=NULL) == call(paged(T=0), starts=FAKE, k=NULL) == 0
+
+
+def test_read_refusals(L):
+    def call(d, fc=3, fout=102, lens=FAKE, table=FAKE, kc=FAKE, k=FAKE):
+        return L.posit_cache_read(NULL, fc, fout, ctypes.byref(d), lens, table, kc, FAKE, k, FAKE)
+
+    for bad in BAD + (dict(longest=-1),):
+        assert call(paged(**bad)) == EINVAL, bad
+    for bad in TOO_MUCH + (dict(longest=2 ** 31),):
+        assert call(paged(**bad)) == EUNSUPPORTED, bad
+    assert call(paged(), fc=1) == call(paged(), fout=2) == EUNSUPPORTED
+    assert call(paged(), fc=77) == call(paged(), fout=103) == EINVAL
+    assert call(paged(), lens=NULL) == call(paged(), table=NULL) == call(paged(), kc=NULL) == call(paged(), k=NULL) == EINVAL
+    assert call(paged(), kc=ctypes.c_void_p(0x1004)) == EINVAL
+    assert call(paged(longest=0), k=NULL) == call(paged(B=0, T=0), k=NULL) == 0
+
+
+def test_attention_refusals(L):
+    def call(d, fq=3, fc=3, fout=102, q=FAKE, starts=NULL, lens=FAKE, table=FAKE, kc=FAKE, o=FAKE, ws=FAKE, n=1 << 40):
+        return L.posit_attention_paged(NULL, fq, fc, fout, ctypes.byref(d), q, starts, lens, table, kc, FAKE, o, FAKE, ws, n)
+
+    for bad in BAD + (dict(HQ=3), dict(HKV=0), dict(window=-1), dict(sinks=-1), dict(most=-1), dict(longest=-1), dict(scale=float("nan")), dict(scale=float("inf")), dict(ql=-1)):
+        assert call(paged(**bad)) == EINVAL, bad
+    for bad in TOO_MUCH + (dict(most=513), dict(most=2 ** 40), dict(longest=2 ** 31)):
+        assert call(paged(**bad)) == EUNSUPPORTED, bad
+    for f in (1, 2, 7, 100, 101):  # posit<16,1>, <32,2>, (12,1), binary32 and binary64 do not fit bfloat16
+        assert call(paged(), fq=f) == EUNSUPPORTED
+    assert call(paged(), fc=1) == call(paged(), fout=2) == EUNSUPPORTED
+    assert call(paged(), fc=77) == call(paged(), fq=103) == call(paged(), fout=103) == call(paged(T=4)) == EINVAL
+    assert call(paged(), q=NULL) == call(paged(), lens=NULL) == call(paged(), table=NULL) == call(paged(), kc=NULL) == call(paged(), o=NULL) == EINVAL
+    assert call(paged(), kc=ctypes.c_void_p(0x1008)) == EINVAL
+    assert call(paged(T=0, B=0), q=NULL) == call(paged(most=0), q=NULL) == 0
+    long = dict(columns=1000, pitch=1000, longest=16000)
+    need = L.posit_attention_paged_workspace(ctypes.byref(paged(**long)))
+    assert need > 0
+    assert call(paged(**long), n=need - 1) == call(paged(**long), ws=NULL) == EWORKSPACE
+    assert call(paged(**long), ws=ctypes.c_void_p(0x1004)) == EINVAL
+    # a window and sinks beyond the cache plan as none
+    for window in (16000, 2 ** 40, 2 ** 63 - 1):
+        for sinks in (0, 2 ** 40, 2 ** 63 - 1):
+            assert L.posit_attention_paged_workspace(ctypes.byref(paged(window=window, sinks=sinks, **long))) == need
+
+
+def test_sample_refusals(L):
+    def call(fz=1, rows=4, vocab=100, z=FAKE, ldz=100, u=FAKE, token=FAKE):
+        return L.posit_sample(NULL, fz, rows, vocab, z, ldz, u, NULL, NULL, NULL, NULL, token, NULL, NULL, NULL, 0)
+
+    assert call(fz=2) == call(fz=101) == EUNSUPPORTED
+    assert call(fz=77) == call(fz=103) == EINVAL
+    assert call(rows=-1) == call(vocab=-1) == call(ldz=99) == EINVAL
+    assert call(z=NULL) == call(u=NULL) == call(token=NULL) == EINVAL
+    assert call(rows=2 ** 31) == call(vocab=2 ** 31, ldz=2 ** 31) == EUNSUPPORTED
+    assert call(rows=0, z=NULL) == call(vocab=0, z=NULL) == 0
+
+
+def test_the_binding_refuses_wrong_tensors():
+    import paper_2105_00053_amd as pn
+    x, w = torch.zeros((2, 3, 16), dtype=torch.uint8), torch.zeros(16)
+    ints = torch.zeros((2, 1), dtype=torch.int32)
+    for call in (lambda: pn.posit_qk_norm_rope_fwd(x, None, "p8", "p8"), lambda: pn.posit_qk_norm_rope_bwd(x, None, x, None, None, "p8", "p8", "p8"),
+                 lambda: pn.posit_cache_append(x, x, x, x, ints, ints[:, 0], "p8", "p8"), lambda: pn.posit_cache_read(x, x, ints, ints[:, 0], 4, 16, "p8", "f32"),
+                 lambda: pn.posit_attention_paged(x, x, x, ints, ints[:, 0], "p8", "p8", "f32"), lambda: pn.posit_sample(w[None], w[:1], "f32"),
+                 lambda: pn.posit_sample(w, w, "f32"), lambda: pn.posit_qk_norm_rope_fwd(w, None, "f32", "f32")):
+        with pytest.raises(pn.PositError):
+            call()
+
+
+def test_the_plain_forms_agree_with_each_other():
+    """The oracle's format of 4 bits: its own values come back, a block's largest element is off by half a step of its binade at most, ties go to even codes."""
+    import generate_util as gu
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((200, 80)) * np.exp2(rng.integers(-40, 40, (200, 1)))
+    codes, powers = gu.f4_encode(x)
+    back = gu.f4_decode(codes, powers)
+    again = gu.f4_encode(back)
+    assert np.array_equal(np.abs(gu.f4_decode(*again)), np.abs(back))
+    step = np.exp2(np.floor(np.log2(np.abs(x)))) / 4
+    grain = np.repeat(np.exp2(powers - 127.0), 32, axis=1)[:, :80]
+    assert (np.abs(back - x) <= np.maximum(step, grain / 4)).all()
+    ties = np.zeros((1, 32))
+    ties[0, :8] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, -5]
+    codes, powers = gu.f4_encode(ties)
+    assert powers[0, 0] == 127 and codes[0, :8].tolist() == [7, 0, 2, 2, 4, 4, 6, 14]
+    assert gu.f4_encode(np.full((1, 32), 7.0))[1][0, 0] == 127 and gu.f4_encode(np.full((1, 32), np.nextafter(7.0, 8)))[1][0, 0] == 128
