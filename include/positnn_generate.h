@@ -97,7 +97,7 @@ size_t posit_attention_paged_workspace(const pnn_paged_desc* desc);
  *   logprob: log of its share in that sum;  kept: how many stay
  * temperature, top_k (int32), top_p, min_p are one value per row, each may be NULL (1, 0, 1, 0).  A temperature of 0 takes the first token; one below 0 or NaN gives token -1 and
  * logprob NaN.  u is one binary32 per row; below 0 and NaN count as 0, what is not below 1 as the largest number below it.  Weights are rounded to multiples of 2^-s, s =
- * min(51, 62 - ceil(log2(vocab))), and their sums are exact.
+ * min(51, 62 - ceil(log2(vocab))), and their sums are exact; a min_p below 2^(-s-2) counts as 0.
  * A row with a NaN or +inf gives token -1, logprob NaN, kept 0; one of -inf alone -1, -inf and 0.  token (int32), logprob and kept (int32; each but token may be NULL) are one
  * value per row.  vocab and rows below 2^31 (else PNN_EUNSUPPORTED). */
 int posit_sample(void* stream, int fz, int64_t rows, int64_t vocab, const void* logits, int64_t ldz, const float* u, const float* temperature, const int32_t* top_k,
