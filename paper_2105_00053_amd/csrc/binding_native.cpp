@@ -387,6 +387,7 @@ PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }  // namespace
 
 #include "binding_lm.h"
+#include "binding_generate.h"
 
 namespace {
 
@@ -396,7 +397,9 @@ PyMethodDef methods[] = {PNN_METHOD("init", init), PNN_METHOD("gemm", gemm), PNN
                          PNN_METHOD("maxpool_bwd", maxpool_bwd), PNN_METHOD("avgpool", avgpool),
                          PNN_METHOD("init_lm", init_lm), PNN_METHOD("rmsnorm_fwd", rmsnorm_fwd), PNN_METHOD("rmsnorm_bwd", rmsnorm_bwd), PNN_METHOD("scale_rows", scale_rows),
                          PNN_METHOD("attention_fwd", attention_fwd), PNN_METHOD("attention_bwd", attention_bwd), PNN_METHOD("logprob_fwd", logprob_fwd),
-                         PNN_METHOD("logprob_bwd", logprob_bwd), {nullptr, nullptr, 0, nullptr}};
+                         PNN_METHOD("logprob_bwd", logprob_bwd), PNN_METHOD("init_generate", init_generate), PNN_METHOD("heads_fwd", heads_fwd),
+                         PNN_METHOD("heads_bwd", heads_bwd), PNN_METHOD("cache_append", cache_append), PNN_METHOD("cache_read", cache_read),
+                         PNN_METHOD("attention_paged", attention_paged), PNN_METHOD("sample", sample), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "positnn_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

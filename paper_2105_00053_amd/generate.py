@@ -11,7 +11,7 @@ import torch
 
 from . import binding
 from .binding import PositError, _check, _stream, load
-from .lm import BF16, _code as _lm_code, _dtype, _ptr, _returned, _vector, _work
+from .lm import _code as _lm_code, _dtype, _ptr, _returned, _vector, _work
 
 F4 = 103
 
@@ -49,8 +49,23 @@ def _load():
             getattr(L, name).restype = ci
         for name in ("posit_qk_norm_rope_bwd_workspace", "posit_attention_paged_workspace", "posit_sample_workspace"):
             getattr(L, name).restype = sz
+        if binding._native is not None:
+            binding._native.init_generate(*(ctypes.cast(getattr(L, name), vp).value for name in _NATIVE_ORDER))
         _lib = L
     return _lib
+
+
+# As in lm.py, a call goes to the extension module first, which returns None for whatever it does not take.
+_NATIVE_ORDER = ("posit_qk_norm_rope_fwd", "posit_qk_norm_rope_bwd", "posit_qk_norm_rope_bwd_workspace", "posit_cache_append", "posit_cache_read", "posit_attention_paged",
+                 "posit_attention_paged_workspace", "posit_sample", "posit_sample_workspace")
+
+
+def _ready():
+    """(the extension module, the current stream, the current device), or three times None where the Python code takes the call."""
+    if _lib is None:
+        _load()
+    stream = binding._ready()
+    return (None, None, None) if stream is None else (binding._native, stream, binding._current_device())
 
 
 def _code(f):
@@ -117,6 +132,11 @@ def posit_qk_norm_rope_fwd(q, k, fx, fy, positions=None, inv_freq=None, wq=None,
     (with positions and inv_freq).  rstd [rows][heads of q, then of k] is None without norm."""
     fx, fy = _code(fx), _code(fy)
     fw = fx if fw is None else _code(fw)
+    native, st, dev = _ready()
+    if native is not None:
+        r = native.heads_fwd(st, dev, fx, fw, fy, 1 if neighbours else 0, float(eps), q, k, wq, wk, positions, inv_freq)
+        if r is not None:
+            return _returned(r)
     desc, qp, kp, wqp, wkp, pp, fp = _heads(q, k, fx, positions, inv_freq, wq, wk, fw, neighbours, eps)
     yq = torch.empty(q.shape, dtype=_dtype(fy), device=q.device)
     yk = None if k is None else torch.empty(k.shape, dtype=_dtype(fy), device=q.device)
@@ -130,6 +150,11 @@ def posit_qk_norm_rope_bwd(dyq, dyk, q, k, rstd, fd, fx, fdx, positions=None, in
     """(dq, dk, dwq, dwk) for the gradients dyq and dyk of the outputs; q, k and rstd as the forward call took and returned them.  dwq and dwk are None without norm."""
     fd, fx, fdx, fdw = _code(fd), _code(fx), _code(fdx), _code(fdw)
     fw = fx if fw is None else _code(fw)
+    native, st, dev = _ready()
+    if native is not None and workspace is None:
+        r = native.heads_bwd(st, dev, fd, fx, fw, fdx, fdw, (1 if neighbours else 0) | (2 if want_dw else 0), dyq, dyk, q, k, wq, wk, positions, inv_freq, rstd)
+        if r is not None:
+            return _returned(r)
     desc, qp, kp, wqp, wkp, pp, fp = _heads(q, k, fx, positions, inv_freq, wq, wk, fw, neighbours, 0.0)
     gqp, desc.gql, desc.gqh = _rows_of_heads(dyq, fd, "dyq", q.shape)
     gkp = None
@@ -193,6 +218,11 @@ def posit_cache_append(k, v, pages_k, pages_v, table, lens, fx, fcache, starts=N
     None without one.  starts [sequences + 1]: first row of each; None for one row each."""
     fx, fcache = _code(fx), _code(fcache)
     fw, fq = fx if fw is None else _code(fw), fx if fq is None else _code(fq)
+    native, st, dev = _ready()
+    if native is not None:
+        r = native.cache_append(st, dev, fx, fw, fq, fcache, 1 if neighbours else 0, float(eps), k, v, pages_k, pages_v, table, lens, starts, q, inv_freq, wq, wk)
+        if r is not None:
+            return _returned(r)[0]
     kp, kl, kh = _rows_of_heads(k, fx, "k")
     rows, hkv, d = k.shape
     vp, vl, vh = _rows_of_heads(v, fx, "v", k.shape)
@@ -217,6 +247,11 @@ def posit_cache_append(k, v, pages_k, pages_v, table, lens, fx, fcache, starts=N
 def posit_cache_read(pages_k, pages_v, table, lens, longest, d, fcache, fout):
     """(k, v) [sequences][longest][heads][d] in fout of what the pages hold; zeros behind a sequence's end."""
     fcache, fout = _code(fcache), _code(fout)
+    native, st, dev = _ready()
+    if native is not None:
+        r = native.cache_read(st, dev, longest, d, fcache, fout, pages_k, pages_v, table, lens, None)
+        if r is not None:
+            return _returned(r)
     if not isinstance(pages_k, torch.Tensor) or pages_k.dim() != 3:
         raise PositError("pages_k must be [pages][heads][elements of a page]")
     hkv = pages_k.shape[1]
@@ -237,6 +272,12 @@ def posit_attention_paged(q, pages_k, pages_v, table, lens, fq, fcache, fout, lo
     """(o [rows][heads][elements], lse [rows][heads]) of the rows q over their sequences' pages.  starts [sequences + 1]: first row of each; None for one row each.  `longest`
     bounds lens (None: what the table holds), `most` the rows of a sequence; scale: 1 / sqrt(elements) by default."""
     fq, fcache, fout = _code(fq), _code(fcache), _code(fout)
+    native, st, dev = _ready()
+    if native is not None and workspace is None and isinstance(q, torch.Tensor) and q.dim() == 3:
+        r = native.attention_paged(st, dev, fq, fcache, fout, most, window, sinks, 1.0 / math.sqrt(max(q.shape[2], 1)) if scale is None else float(scale), q, pages_k, pages_v, table, lens,
+                                   starts, longest)
+        if r is not None:
+            return _returned(r)
     qp, ql, qh = _rows_of_heads(q, fq, "q")
     rows, hq, d = q.shape
     if not isinstance(pages_k, torch.Tensor) or pages_k.dim() != 3:
@@ -261,6 +302,11 @@ def posit_attention_paged(q, pages_k, pages_v, table, lens, fq, fcache, fout, lo
 def posit_sample(logits, u, fz, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None):
     """(token, logprob, kept) for each row of logits from u, one number from 0 to 1 each; the limits are a value per row, or None."""
     fz = _code(fz)
+    native, st, dev = _ready()
+    if native is not None and workspace is None:
+        r = native.sample(st, dev, fz, logits, u, temperature, top_k, top_p, min_p)
+        if r is not None:
+            return _returned(r)
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
         raise PositError("logits must be a 2-D tensor")
     zp = _ptr(logits, fz, "logits")
