@@ -4,7 +4,7 @@
 namespace pnn {
 
 struct PagedPlan {
-    int blocks, tiles, parts;
+    int rows, blocks, tiles, parts;
     int64_t bytes;
 };
 
@@ -23,7 +23,8 @@ inline int64_t paged_keys(const pnn_paged_desc& d) { return d.longest < d.column
 inline PagedPlan paged_plan(const pnn_paged_desc& d) {
     PagedPlan p = {};
     const int64_t G = d.HQ / d.HKV, longest = paged_keys(d);
-    p.blocks = (int)((d.most * G + 15) / 16);
+    p.rows = d.most * G <= 4 ? 4 : (d.most * G <= 8 ? 8 : 16);
+    p.blocks = (int)((d.most * G + p.rows - 1) / p.rows);
     int64_t keys = longest;
     const int64_t window = d.window < longest ? d.window : 0, sinks = d.sinks < longest ? d.sinks : longest;  // both small: their sum is
     if (window > 0 && window + d.most + sinks + 64 < keys) keys = window + d.most + sinks + 64;
@@ -35,18 +36,29 @@ inline PagedPlan paged_plan(const pnn_paged_desc& d) {
     p.tiles = (int)((all + parts - 1) / parts);
     p.tiles = (p.tiles + 3) / 4 * 4;
     p.parts = (int)((all + p.tiles - 1) / p.tiles);
-    p.bytes = p.parts > 1 ? groups * p.parts * 16 * (d.D + 2) * 4 : 0;
+    p.bytes = p.parts > 1 ? groups * p.parts * p.rows * (d.D + 2) * 4 : 0;
     return p;
 }
 
-template <int KC>
-void launch_paged(hipStream_t st, int db, const dim3& grid, const AttnPaged& a) {
-    switch (db) {
-        case 1: hipLaunchKernelGGL((attn_paged_kernel<KC, 1>), grid, dim3(256), 0, st, a); break;
-        case 2: hipLaunchKernelGGL((attn_paged_kernel<KC, 2>), grid, dim3(256), 0, st, a); break;
-        case 3: hipLaunchKernelGGL((attn_paged_kernel<KC, 3>), grid, dim3(256), 0, st, a); break;
-        default: hipLaunchKernelGGL((attn_paged_kernel<KC, 4>), grid, dim3(256), 0, st, a); break;
+template <int KC, int ROWS>
+void launch_paged(hipStream_t st, const dim3& grid, const AttnPaged& a) {
+    const bool full = a.n.D % 32 == 0;
+#define PNN_PAGED(DB)                                                                                              \
+    if (full) hipLaunchKernelGGL((attn_paged_kernel<KC, DB, ROWS, true>), grid, dim3(256), 0, st, a);              \
+    else hipLaunchKernelGGL((attn_paged_kernel<KC, DB, ROWS, false>), grid, dim3(256), 0, st, a);
+    switch ((a.n.D + 31) / 32) {
+        case 1: PNN_PAGED(1) break;
+        case 2: PNN_PAGED(2) break;
+        case 3: PNN_PAGED(3) break;
+        default: PNN_PAGED(4) break;
     }
+#undef PNN_PAGED
+}
+template <int KC>
+void launch_paged(hipStream_t st, const dim3& grid, const AttnPaged& a) {
+    if (a.rows == 4) launch_paged<KC, 4>(st, grid, a);
+    else if (a.rows == 8) launch_paged<KC, 8>(st, grid, a);
+    else launch_paged<KC, 16>(st, grid, a);
 }
 
 }  // namespace pnn
@@ -83,15 +95,14 @@ extern "C" int posit_attention_paged(void* stream, int fq, int fcache, int fout,
     a.n.HKV = (int)d.HKV; a.n.G = (int)(d.HQ / d.HKV); a.n.D = (int)d.D; a.n.scale = d.scale;
     a.q = q; a.k = (const char*)k_pages; a.v = (const char*)v_pages; a.ql = d.ql; a.qh = d.qh; a.kq = kind_of(fq); a.most = (int)d.most; a.fq = elem_fmt(fq); a.fc = elem_fmt(fcache);
     a.o = o; a.lse = lse; a.ko = kind_of(fout); a.fo = elem_fmt(fout);
-    a.blocks = p.blocks; a.tiles = p.tiles; a.parts = p.parts; a.part = (float*)workspace;
+    a.rows = p.rows; a.blocks = p.blocks; a.tiles = p.tiles; a.parts = p.parts; a.part = (float*)workspace;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
     const dim3 grid((unsigned)(p.blocks * p.parts), (unsigned)d.HKV, (unsigned)d.B);
-    const int db = (int)((d.D + 31) / 32);
     switch (cache_kind(fcache)) {
-        case CACHE_U8: launch_paged<CACHE_U8>(st, db, grid, a); break;
-        case CACHE_BF16: launch_paged<CACHE_BF16>(st, db, grid, a); break;
-        default: launch_paged<CACHE_F4>(st, db, grid, a); break;
+        case CACHE_U8: launch_paged<CACHE_U8>(st, grid, a); break;
+        case CACHE_BF16: launch_paged<CACHE_BF16>(st, grid, a); break;
+        default: launch_paged<CACHE_F4>(st, grid, a); break;
     }
     if (p.parts > 1) hipLaunchKernelGGL(attn_paged_join_kernel, dim3((unsigned)(d.most * a.n.G), (unsigned)d.HKV, (unsigned)d.B), dim3(128), 0, st, a);
     return hip_status(hipGetLastError());

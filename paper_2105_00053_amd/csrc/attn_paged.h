@@ -24,9 +24,9 @@ struct AttnPaged {
     float* lse;
     int ko;
     ElemFmt fo;
-    int blocks;           // row blocks of 16
+    int rows, blocks;     // of a row block; row blocks
     int tiles, parts;     // of a part; workgroups that a row block's keys are split over
-    float* part;          // [row block][part][m: 16][l: 16][16][D]
+    float* part;          // [row block][part][m: rows][l: rows][rows][D]
 };
 
 // A sequence's rows and keys
@@ -44,7 +44,7 @@ struct PagedRows {
 };
 
 // A tile's keys and values as they lie in memory
-template <int KC, int KS, int NV>
+template <int KC, int KS>
 struct PagedRaw {
     static constexpr int KW = KC == CACHE_F4 ? 1 : (KC == CACHE_U8 ? 2 : 4);  // words of eight elements
     uint32_t k[2][KS * KW], v[2][4 * KW];
@@ -52,10 +52,29 @@ struct PagedRaw {
     bool bad[2];  // the halves' pages are none
 };
 
-template <int KC, int DB>
+// Of a value that stands in the lanes N further up in the row of 16, or down (zero where there is none)
+template <int N>
+__device__ __forceinline__ uint32_t from_above(uint32_t v) { return lane_shift<0x100 + N, 0xF>(v, 0u); }
+// v of the lane's row N further down in the banks (of four lanes) of BANKS, `own` elsewhere
+template <int N, int BANKS>
+__device__ __forceinline__ float spread(float own, float v) {
+    return f32_of_bits((uint32_t)__builtin_amdgcn_update_dpp((int)bits_of_f32(own), (int)bits_of_f32(v), 0x110 + N, 0xF, BANKS, false));
+}
+template <int N>
+__device__ __forceinline__ float turned(float v) { return f32_of_bits(lane_shift<0x120 + N, 0xF>(bits_of_f32(v), 0u)); }
+// the larger of a lane's value and that of the lane 16 away
+__device__ __forceinline__ float max_rows(float v) {
+    typedef uint32_t v2 __attribute__((ext_vector_type(2)));
+    const v2 r = __builtin_amdgcn_permlane16_swap(bits_of_f32(v), bits_of_f32(v), false, false);
+    return fmaxf(f32_of_bits(r.x), f32_of_bits(r.y));
+}
+
+// ROWS: of a block (4, 8 or 16).  The first product has 16 columns, one to a lane of 16, and four lanes have a column; of fewer rows the scores go to the lanes whose columns
+// are none, so that each works on 8 ROWS / 16 of them.  FULL: heads of 32 DB elements.
+template <int KC, int DB, int ROWS, bool FULL>
 __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kernel(AttnPaged a) {
-    constexpr int KS = DB, NV = DB <= 2 ? 4 : 8;
-    typedef PagedRaw<KC, KS, NV> R;
+    constexpr int KS = DB, NV = DB <= 2 ? 4 : 8, SC = ROWS / 2;
+    typedef PagedRaw<KC, KS> R;
     __shared__ uint32_t smem[8192];  // the table, then what the waves join through
     __shared__ float wm[4][16], wl[4][16];
     const CacheShape& s = a.s;
@@ -64,19 +83,20 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     const int hk = blockIdx.y, b = blockIdx.z;
     const int rb = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - rb * a.parts;
     const PagedRows x(a, b);
-    if (rb * 16 >= x.rows) return;
-    const int row = rb * 16 + col, last = rb * 16 + 15 < x.rows ? rb * 16 + 15 : x.rows - 1;
+    if (rb * ROWS >= x.rows) return;
+    const int row = rb * ROWS + col % ROWS, last = rb * ROWS + ROWS - 1 < x.rows ? rb * ROWS + ROWS - 1 : x.rows - 1;
     const int i = row / n.G, h = hk * n.G + (row - i * n.G);
     const bool live = row < x.rows;
     const int p = live ? x.base + i : -1, low = n.window ? p - n.window : -1;
-    const int p0 = x.base + rb * 16 / n.G, p1 = x.base + last / n.G;
+    const int p0 = x.base + rb * ROWS / n.G, p1 = x.base + last / n.G;
     const int low1 = n.window ? p1 - n.window : -1;
     const AttnTiles tiles = at_tiles<32>(n, p0, p1);
     const int begin = part * a.tiles, end = begin + a.tiles < tiles.count ? begin + a.tiles : tiles.count;
     if (a.parts > 1 && part > 0 && begin >= tiles.count) return;
     const int keys = x.keys, D = n.D;
 
-    auto key_of = [&](int i) { return 16 * (i >> 2) + 4 * quarter + (i & 3); };  // the lane's i-th key of a tile, as scores and as values
+    auto key_of = [&](int i) { return 16 * (i >> 2) + 4 * quarter + (i & 3); };  // the lane's i-th key of a tile, as values
+    auto score_of = [&](int i) { return key_of(col / ROWS * SC + i); };           // and as the scores that it works on
     // the pages of a tile's halves; the last key's in place of those behind it
     auto page_of = [&](int m, int half) -> int64_t {
         const int key = tiles.at(m) * 32 + 16 * half;
@@ -93,24 +113,36 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
             const char* const vp = a.v + page;
             // of a key, the lane's run of 8 KS elements
             const int at = at0 + col;
+            if (FULL) {
+                const int el = cache_unit(s, false, at, KS * quarter);
+                __builtin_memcpy(r.k[y], kp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 4 * R::KW * KS);
+                if (KC == CACHE_F4) {
+                    const char* const powers = kp + cache_power(s, false, at, 0);
+                    const uint32_t first = ((const uint8_t*)powers)[KS * quarter >> 2];
+                    const uint32_t last = DB == 3 ? ((const uint8_t*)powers)[(KS * quarter + KS - 1) >> 2] : first;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int unit = KS * quarter + ks, el = cache_unit(s, false, at, 8 * unit < D ? unit : 0);
-                __builtin_memcpy(&r.k[y][ks * R::KW], kp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 4 * R::KW);
-                if (KC == CACHE_F4) r.kp[y][ks] = ((const uint8_t*)kp)[cache_power(s, false, at, 8 * unit < D ? unit >> 2 : 0)];
+                    for (int ks = 0; ks < KS; ++ks) r.kp[y][ks] = DB == 3 && (KS * quarter + ks) >> 2 != KS * quarter >> 2 ? last : first;
+                }
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const int unit = KS * quarter + ks, el = cache_unit(s, false, at, 8 * unit < D ? unit : 0);
+                    __builtin_memcpy(&r.k[y][ks * R::KW], kp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 4 * R::KW);
+                    if (KC == CACHE_F4) r.kp[y][ks] = ((const uint8_t*)kp)[cache_power(s, false, at, 8 * unit < D ? unit >> 2 : 0)];
+                }
             }
             // of four tokens' values, the lane's block of eight elements (a half of it where NV is 4)
-            const int unit = NV * col / 8 < D / 8 ? NV * col / 8 : 0, el = cache_unit(s, true, at0 + 4 * quarter, unit);
+            const int unit = FULL || NV * col / 8 < D / 8 ? NV * col / 8 : 0, el = cache_unit(s, true, at0 + 4 * quarter, unit);
             __builtin_memcpy(r.v[y], vp + (KC == CACHE_F4 ? el / 2 : KC == CACHE_U8 ? el : 2 * el), 16 * R::KW);
             if (KC == CACHE_F4) __builtin_memcpy(&r.vp[y], vp + cache_power(s, true, at0 + 4 * quarter, unit >> 2), 4);
         }
     };
-    R raw;
+    R even, odd;
     int64_t pages[2] = {-1, -1};
     if (begin + w < end) {
         pages[0] = page_of(begin + w, 0);
         pages[1] = page_of(begin + w, 1);
-        load(begin + w, pages, raw);
+        load(begin + w, pages, even);
         if (begin + w + 4 < end) {
             pages[0] = page_of(begin + w + 4, 0);
             pages[1] = page_of(begin + w + 4, 1);
@@ -133,7 +165,7 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     for (int ks = 0; ks < KS; ++ks) {
         const int d = 8 * (KS * quarter + ks);
         uint4 u = make_uint4(0, 0, 0, 0);
-        if (live && d < D) u = at_load8(a.q, (int64_t)(x.first + i) * a.ql + h * a.qh + d, 8, a.kq, a.fq);
+        if (live && col < ROWS && d < D) u = at_load8(a.q, (int64_t)(x.first + i) * a.ql + h * a.qh + d, 8, a.kq, a.fq);
         q[ks] = at_scaled(u, c);
     }
     c = at_scale(c);
@@ -151,8 +183,7 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
         if constexpr (KC == CACHE_F4) {
             uint32_t o[4];
             four(e[0], f4_scale(power), o);
-            const uint32_t nan = power == 255u ? 0x7FC07FC0u : 0u;
-            return make_uint4(o[0] | nan, o[1] | nan, o[2] | nan, o[3] | nan);
+            return make_uint4(o[0], o[1], o[2], o[3]);
         } else if constexpr (KC == CACHE_U8) {
             auto two = [&](uint32_t word, int i) { return __builtin_amdgcn_perm(entry(word, i + 1), entry(word, i), 0x05040100u); };
             return make_uint4(two(e[0], 0), two(e[0], 2), two(e[1], 0), two(e[1], 2));
@@ -167,38 +198,66 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
 #pragma unroll
     for (int y = 0; y < NV; ++y) o[y] = at_v4f{0.f, 0.f, 0.f, 0.f};
     uint32_t flagged = 0;
-    for (int tile = begin + w; tile < end; tile += 4) {
-        const R cur = raw;
+    auto step = [&](int tile, const R& cur, R& next) {
         if (tile + 4 < end) {
-            load(tile + 4, pages, raw);
+            load(tile + 4, pages, next);
             if (tile + 8 < end) {
                 pages[0] = page_of(tile + 8, 0);
                 pages[1] = page_of(tile + 8, 1);
             }
         }
         const int key0 = tiles.at(tile) * 32;
-        float sc[8];  // of keys key_of(0 .. 7)
+        float all[8];  // of keys key_of(0 .. 7)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             at_v4f acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 uint4 u = key_words(&cur.k[y][ks * R::KW], KC == CACHE_F4 ? cur.kp[y][ks] : 0u);
-                if (D < 32 * DB) u = 8 * (KS * quarter + ks) < D ? u : make_uint4(0, 0, 0, 0);
+                if (!FULL) u = 8 * (KS * quarter + ks) < D ? u : make_uint4(0, 0, 0, 0);
                 acc = at_mfma16(at_frag(u), q[ks], acc);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sc[4 * y + r] = cur.bad[y] ? nan : acc[r];
+            for (int r = 0; r < 4; ++r) all[4 * y + r] = acc[r];
+        }
+        // pages that are none; blocks of NaN, a block of a key to a lane
+        if (cur.bad[0] || cur.bad[1]) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) all[r] = cur.bad[r >> 2] ? nan : all[r];
+        }
+        if (KC == CACHE_F4) {
+            bool gone[2] = {false, false};
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) gone[y] |= cur.kp[y][ks] == 255u;
+            if (__any(gone[0] || gone[1])) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint64_t lanes = __ballot(gone[y]);
+                    const uint32_t keys16 = (uint32_t)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) all[4 * y + r] = (keys16 >> (4 * quarter + r)) & 1u ? nan : all[4 * y + r];
+                }
+            }
+        }
+        float sc[SC];  // of keys score_of(0 ..)
+#pragma unroll
+        for (int r = 0; r < SC; ++r) {
+            sc[r] = all[r];
+            if (ROWS == 8) sc[r] = spread<8, 0xC>(sc[r], all[(SC + r) & 7]);
+            if (ROWS == 4) sc[r] = spread<12, 0x8>(spread<8, 0x4>(spread<4, 0x2>(sc[r], all[(2 + r) & 7]), all[(4 + r) & 7]), all[(6 + r) & 7]);
         }
         if (!(key0 + 31 <= p0 && (key0 > low1 || key0 + 31 < n.sinks))) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r) sc[r] = at_sees(n, p, low, key0 + key_of(r)) ? sc[r] : -inf;
+            for (int r = 0; r < SC; ++r) sc[r] = at_sees(n, p, low, key0 + score_of(r)) ? sc[r] : -inf;
         }
         float mx = sc[0];
 #pragma unroll
-        for (int r = 1; r < 8; ++r) mx = fmaxf(mx, sc[r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = at_max_halves(mx) * c;
+        for (int r = 1; r < SC; ++r) mx = fmaxf(mx, sc[r]);
+        if (ROWS <= 8) mx = fmaxf(mx, turned<8>(mx));
+        if (ROWS <= 4) mx = fmaxf(mx, turned<4>(mx));
+        mx = at_max_halves(max_rows(mx)) * c;
         if (__any(mx > m + 8.f)) {
             const float m1 = fmaxf(m, mx), f = m1 == -inf ? 1.f : __builtin_amdgcn_exp2f(m - m1);
             m = m1;
@@ -208,16 +267,35 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
         }
         const float mr = m == -inf ? 0.f : m;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < SC; ++r) {
             sc[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -mr));
             l += sc[r];
         }
-        at_v8b ph, pl;
+        // the probabilities in two parts, back to the lanes whose columns they are
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            ph[r] = (__bf16)sc[r];
-            pl[r] = (__bf16)(sc[r] - (float)ph[r]);
+        for (int r = 0; r < SC / 2; ++r) {
+            v2b h = {(__bf16)sc[2 * r], (__bf16)sc[2 * r + 1]};
+            hi[r] = __builtin_bit_cast(uint32_t, h);
+            v2b g = {(__bf16)(sc[2 * r] - f32_of_bits(hi[r] << 16)), (__bf16)(sc[2 * r + 1] - f32_of_bits(hi[r] & 0xFFFF0000u))};
+            lo[r] = __builtin_bit_cast(uint32_t, g);
         }
+        if (ROWS == 8) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                hi[2 + r] = from_above<8>(hi[r]);
+                lo[2 + r] = from_above<8>(lo[r]);
+            }
+        }
+        if (ROWS == 4) {
+            hi[1] = from_above<4>(hi[0]);
+            hi[2] = from_above<8>(hi[0]);
+            hi[3] = from_above<12>(hi[0]);
+            lo[1] = from_above<4>(lo[0]);
+            lo[2] = from_above<8>(lo[0]);
+            lo[3] = from_above<12>(lo[0]);
+        }
+        const at_v8b ph = at_frag(make_uint4(hi[0], hi[1], hi[2], hi[3])), pl = at_frag(make_uint4(lo[0], lo[1], lo[2], lo[3]));
 
         // what lies behind the last key is anything: zeros
         uint32_t v[2][4 * R::KW], vp[2];
@@ -239,26 +317,26 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
                 }
         }
         // NaR, NaN and infinities: zeros, and looked up at the end
-        uint32_t odd = 0;
+        uint32_t special = 0;
         if (KC == CACHE_F4) {
 #pragma unroll
-            for (int y = 0; y < 2; ++y) odd |= (~vp[y] - 0x01010101u) & vp[y] & 0x80808080u;
+            for (int y = 0; y < 2; ++y) special |= (~vp[y] - 0x01010101u) & vp[y] & 0x80808080u;
         } else if (KC == CACHE_U8) {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t z = v[y][e] ^ 0x80808080u;
-                    odd |= (z - 0x01010101u) & ~z & 0x80808080u;
+                    special |= (z - 0x01010101u) & ~z & 0x80808080u;
                 }
         } else {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) odd |= at_odd(v[y][e]) ? 1u : 0u;
+                for (int e = 0; e < 16; ++e) special |= at_odd(v[y][e]) ? 1u : 0u;
         }
-        flagged |= odd;
-        if (KC != CACHE_U8 && __any(odd != 0)) {
+        flagged |= special;
+        if (KC != CACHE_U8 && __any(special != 0)) {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -326,7 +404,13 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
                 o[y] = at_mfma16(f, pl, o[y]);
             }
         }
+    };
+    for (int tile = begin + w; tile < end; tile += 8) {
+        step(tile, even, odd);
+        if (tile + 4 < end) step(tile + 4, odd, even);
     }
+    if (ROWS <= 8) l += turned<8>(l);
+    if (ROWS <= 4) l += turned<4>(l);
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (__any(flagged != 0)) {
@@ -375,12 +459,13 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     }
 
     // join the waves: a common reference, then through LDS, [wave][block][element row][column]
-    if (quarter == 0) {
+    if (quarter == 0 && col < ROWS) {
         wm[w][col] = m;
         wl[w][col] = l;
     }
     __syncthreads();
-    const float top = fmaxf(fmaxf(wm[0][col], wm[1][col]), fmaxf(wm[2][col], wm[3][col]));
+    const int cr = col % ROWS;
+    const float top = fmaxf(fmaxf(wm[0][cr], wm[1][cr]), fmaxf(wm[2][cr], wm[3][cr]));
     const float f = m == -inf ? 1.f : __builtin_amdgcn_exp2f(m - top);
     float* const red = (float*)smem;
 #pragma unroll
@@ -392,8 +477,8 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
         }
     __syncthreads();
     // NV neighbouring elements of a row to a thread
-    const int rr = t >> 4, rho = t & 15, gr = rb * 16 + rr, d = NV * rho;
-    if (gr >= x.rows) return;
+    const int rr = t >> 4, rho = t & 15, gr = rb * ROWS + rr, d = NV * rho;
+    if (rr >= ROWS || gr >= x.rows) return;
     float out[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int y = 0; y < NV; ++y)
@@ -405,14 +490,14 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
 #pragma unroll
     for (int z = 0; z < 4; ++z) sum += wm[z][rr] == -inf ? wl[z][rr] : wl[z][rr] * __builtin_amdgcn_exp2f(wm[z][rr] - mm);
     if (a.parts > 1 && tiles.count > a.tiles) {
-        float* const at = a.part + ((((int64_t)b * s.HKV + hk) * a.blocks + rb) * a.parts + part) * (16 * (D + 2));
+        float* const at = a.part + ((((int64_t)b * s.HKV + hk) * a.blocks + rb) * a.parts + part) * (ROWS * (D + 2));
         if (rho == 0) {
             at[rr] = mm;
-            at[16 + rr] = sum;
+            at[ROWS + rr] = sum;
         }
 #pragma unroll
         for (int y = 0; y < NV; ++y)
-            if (d + y < D) at[32 + rr * D + d + y] = out[y];
+            if (d + y < D) at[2 * ROWS + rr * D + d + y] = out[y];
         return;
     }
     const int gi = gr / n.G, gh = hk * n.G + (gr - gi * n.G);
@@ -429,15 +514,15 @@ __global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
     __shared__ float weight[AT_MOST_PARTS];
     __shared__ float half_max[2], half_sum[2];
     const AttnShape& n = a.n;
-    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x, rr = row & 15, rb = row >> 4, D = n.D;
+    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x, rb = row / a.rows, rr = row - rb * a.rows, D = n.D;
     const PagedRows x(a, b);
     if (row >= x.rows) return;
     const int i = row / n.G, h = hk * n.G + (row - i * n.G);
-    const int last = rb * 16 + 15 < x.rows ? rb * 16 + 15 : x.rows - 1;
-    const int count = at_tiles<32>(n, x.base + rb * 16 / n.G, x.base + last / n.G).count;
+    const int last = rb * a.rows + a.rows - 1 < x.rows ? rb * a.rows + a.rows - 1 : x.rows - 1;
+    const int count = at_tiles<32>(n, x.base + rb * a.rows / n.G, x.base + last / n.G).count;
     if (count <= a.tiles) return;
     const int parts = (count + a.tiles - 1) / a.tiles;
-    const int64_t step = 16 * (D + 2);
+    const int64_t step = a.rows * (D + 2);
     const float* const at = a.part + ((((int64_t)b * a.s.HKV + hk) * a.blocks + rb) * a.parts) * step;
     const float inf = f32_of_bits(0x7F800000u);
     float mine[AT_MOST_PARTS / 128], sums[AT_MOST_PARTS / 128], m = -inf, l = 0.f;
@@ -445,7 +530,7 @@ __global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
     for (int y = 0; y < AT_MOST_PARTS / 128; ++y) {
         const int p = t + 128 * y;
         mine[y] = p < parts ? at[p * step + rr] : -inf;
-        sums[y] = p < parts ? at[p * step + 16 + rr] : 0.f;
+        sums[y] = p < parts ? at[p * step + a.rows + rr] : 0.f;
         m = fmaxf(m, mine[y]);
     }
     m = wave_max(m);
@@ -465,7 +550,7 @@ __global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
     const int64_t to = (int64_t)(x.first + i) * (a.s.HKV * n.G) + h;
     if (a.lse && t == 0) a.lse[to] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
     if (t >= D) return;
-    const float* const from = at + 32 + rr * D + t;
+    const float* const from = at + 2 * a.rows + rr * D + t;
     float o = 0.f;
     for (int p = 0; p < parts; p += 8) {
         float v[8];
