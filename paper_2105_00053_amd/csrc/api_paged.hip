@@ -83,7 +83,7 @@ extern "C" int posit_attention_paged(void* stream, int fq, int fcache, int fout,
     if (!q || !lens || (d.columns > 0 && !table) || (d.pages > 0 && (!k_pages || !v_pages)) || !o) return PNN_EINVAL;
     if (!aligned(k_pages, 16) || !aligned(v_pages, 16)) return PNN_EINVAL;
     const PagedPlan p = paged_plan(d);
-    if ((int64_t)p.blocks * p.parts > most_workgroups(256) || d.most * (d.HQ / d.HKV) > most_workgroups(128)) return PNN_EUNSUPPORTED;
+    if ((int64_t)p.blocks * p.parts * d.HKV * d.B > most_workgroups(256) || d.most * (d.HQ / d.HKV) > most_workgroups(512)) return PNN_EUNSUPPORTED;
     if (p.bytes > 0 && (!workspace || workspace_bytes < (size_t)p.bytes)) return PNN_EWORKSPACE;
     if (p.bytes > 0 && !aligned(workspace, 16)) return PNN_EINVAL;
     AttnPaged a = {};
@@ -98,12 +98,12 @@ extern "C" int posit_attention_paged(void* stream, int fq, int fcache, int fout,
     a.rows = p.rows; a.blocks = p.blocks; a.tiles = p.tiles; a.parts = p.parts; a.part = (float*)workspace;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
-    const dim3 grid((unsigned)(p.blocks * p.parts), (unsigned)d.HKV, (unsigned)d.B);
+    const dim3 grid((unsigned)((int64_t)p.blocks * p.parts * d.HKV * d.B));
     switch (cache_kind(fcache)) {
         case CACHE_U8: launch_paged<CACHE_U8>(st, grid, a); break;
         case CACHE_BF16: launch_paged<CACHE_BF16>(st, grid, a); break;
         default: launch_paged<CACHE_F4>(st, grid, a); break;
     }
-    if (p.parts > 1) hipLaunchKernelGGL(attn_paged_join_kernel, dim3((unsigned)(d.most * a.n.G), (unsigned)d.HKV, (unsigned)d.B), dim3(128), 0, st, a);
+    if (p.parts > 1) hipLaunchKernelGGL(attn_paged_join_kernel, dim3((unsigned)(d.most * a.n.G), (unsigned)d.HKV, (unsigned)d.B), dim3(512), 0, st, a);
     return hip_status(hipGetLastError());
 }

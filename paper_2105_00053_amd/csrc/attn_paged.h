@@ -80,8 +80,10 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     const CacheShape& s = a.s;
     const AttnShape& n = a.n;
     const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6), quarter = lane >> 4, col = lane & 15;
-    const int hk = blockIdx.y, b = blockIdx.z;
-    const int rb = blockIdx.x / (unsigned)a.parts, part = blockIdx.x - rb * a.parts;
+    // Heads fastest, then sequences, row blocks, parts: the later parts, which the longer sequences alone have, spread over the chip's eight dies as all others do (with parts fastest, four
+    // of them left two dies without work: 64 sequences of up to 8192 took 104 us where three took 85), and short ones come last.
+    const unsigned heads = (unsigned)s.HKV, groups = heads * s.B;
+    const int part = blockIdx.x / (groups * a.blocks), rb = blockIdx.x / groups % a.blocks, b = blockIdx.x % groups / heads, hk = blockIdx.x % heads;
     const PagedRows x(a, b);
     if (rb * ROWS >= x.rows) return;
     const int row = rb * ROWS + col % ROWS, last = rb * ROWS + ROWS - 1 < x.rows ? rb * ROWS + ROWS - 1 : x.rows - 1;
@@ -509,10 +511,10 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     at_store8(a.o, to * D + d, D - d < NV ? D - d : NV, a.ko, a.fo, out);
 }
 
-// Parts of a row joined, one row to a workgroup and an element to a thread; rows whose keys are in one part are done.
-__global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
+// Parts of a row joined, one row to a workgroup, an element to a thread of each four, which take the parts in turn; rows whose keys are in one part are done.
+__global__ __launch_bounds__(512) void attn_paged_join_kernel(AttnPaged a) {
     __shared__ float weight[AT_MOST_PARTS];
-    __shared__ float half_max[2], half_sum[2];
+    __shared__ float wave_max_of[4], wave_sum_of[4], sums[4][128];
     const AttnShape& n = a.n;
     const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, t = threadIdx.x, rb = row / a.rows, rr = row - rb * a.rows, D = n.D;
     const PagedRows x(a, b);
@@ -525,41 +527,40 @@ __global__ __launch_bounds__(128) void attn_paged_join_kernel(AttnPaged a) {
     const int64_t step = a.rows * (D + 2);
     const float* const at = a.part + ((((int64_t)b * a.s.HKV + hk) * a.blocks + rb) * a.parts) * step;
     const float inf = f32_of_bits(0x7F800000u);
-    float mine[AT_MOST_PARTS / 128], sums[AT_MOST_PARTS / 128], m = -inf, l = 0.f;
+    // a part to a thread of the first four waves
+    const bool mine = t < parts;
+    const float m0 = mine ? at[t * step + rr] : -inf, s0 = mine ? at[t * step + a.rows + rr] : 0.f;
+    // the outputs are on their way meanwhile
+    const int e = t & 127, g = t >> 7;
+    const float* const from = at + 2 * a.rows + rr * D + (e < D ? e : 0);
+    float v[8];
 #pragma unroll
-    for (int y = 0; y < AT_MOST_PARTS / 128; ++y) {
-        const int p = t + 128 * y;
-        mine[y] = p < parts ? at[p * step + rr] : -inf;
-        sums[y] = p < parts ? at[p * step + a.rows + rr] : 0.f;
-        m = fmaxf(m, mine[y]);
-    }
-    m = wave_max(m);
-    if ((t & 63) == 0) half_max[t >> 6] = m;
+    for (int y = 0; y < 8; ++y) v[y] = from[(g + 4 * y < parts ? g + 4 * y : 0) * step];
+    float m = wave_max(m0);
+    if ((t & 63) == 0 && t < 256) wave_max_of[t >> 6] = m;
     __syncthreads();
-    m = fmaxf(half_max[0], half_max[1]);
-#pragma unroll
-    for (int y = 0; y < AT_MOST_PARTS / 128; ++y) {
-        const float f = mine[y] == -inf ? 1.f : __builtin_amdgcn_exp2f(mine[y] - m);  // a part without keys: zeros, or NaN
-        weight[t + 128 * y] = f;
-        l += sums[y] * f;
-    }
-    l = wave_sum(l);
-    if ((t & 63) == 0) half_sum[t >> 6] = l;
+    m = fmaxf(fmaxf(wave_max_of[0], wave_max_of[1]), fmaxf(wave_max_of[2], wave_max_of[3]));
+    const float f = m0 == -inf ? 1.f : __builtin_amdgcn_exp2f(m0 - m);  // a part without keys: zeros, or NaN
+    if (t < AT_MOST_PARTS) weight[t] = f;
+    float l = wave_sum(s0 * f);
+    if ((t & 63) == 0 && t < 256) wave_sum_of[t >> 6] = l;
     __syncthreads();
-    l = half_sum[0] + half_sum[1];
+    l = (wave_sum_of[0] + wave_sum_of[1]) + (wave_sum_of[2] + wave_sum_of[3]);
     const int64_t to = (int64_t)(x.first + i) * (a.s.HKV * n.G) + h;
     if (a.lse && t == 0) a.lse[to] = l == 0.f ? -inf : m * 0.6931471805599453f + logf(l);
-    if (t >= D) return;
-    const float* const from = at + 2 * a.rows + rr * D + t;
     float o = 0.f;
-    for (int p = 0; p < parts; p += 8) {
-        float v[8];
-#pragma unroll
-        for (int y = 0; y < 8; ++y) v[y] = from[(p + y < parts ? p + y : 0) * step];
+    for (int p = g; p < parts; p += 32) {
 #pragma unroll
         for (int y = 0; y < 8; ++y)
-            if (p + y < parts) o += v[y] - v[y] == 0.f ? v[y] * weight[p + y] : v[y];
+            if (p + 4 * y < parts) o += v[y] - v[y] == 0.f ? v[y] * weight[p + 4 * y] : v[y];
+        if (p + 32 < parts)
+#pragma unroll
+            for (int y = 0; y < 8; ++y) v[y] = from[(p + 32 + 4 * y < parts ? p + 32 + 4 * y : 0) * step];
     }
+    sums[g][e] = o;
+    __syncthreads();
+    if (t >= D) return;
+    o = (sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]);
     o = l == 0.f ? 0.f : o / l;
     store_value(a.o, to * D + t, a.ko, a.fo, o);
 }
