@@ -31,7 +31,7 @@ enum { PNN_F4 = 103 };
  *   y_a = t_a cos - t_b sin,  y_b = t_b cos + t_a sin              (pos NULL: y = t); the elements from R on stay
  * q, k in fx; weights in fw; outputs in fy, dense [T][HQ][D] and [T][HKV][D]; rstd (may be NULL) one binary32 per row and head, [T][HQ + HKV], queries
  * first.  inv_freq is R / 2 values of binary64, pos T of int32 (of either sign).
- * D even and at most 256, T below 2^31, HQ + HKV below 65536 (else PNN_EUNSUPPORTED); R even and at most D (else PNN_EINVAL). */
+ * D even and at most 256, T below 2^31, HQ + HKV below 65536, strides below 2^32 (else PNN_EUNSUPPORTED); R even and at most D (else PNN_EINVAL). */
 typedef struct {
     int64_t T, HQ, HKV, D, R;
     int64_t ql, qh, kl, kh;      /* strides of q and k: row, head */
@@ -70,7 +70,8 @@ typedef struct {
 } pnn_paged_desc;
 
 /* q, k and v (fx; strides) of the new tokens: q and k normalised (wq, wk in fw, both or none) and rotated (inv_freq, NULL for none) as above, by a token's place in its sequence; q
- * to yq (fq, dense [T][HQ][D]; q NULL: left out), k and v (as it is) into the pages.  All of it in 64 bits, so that what is stored is the nearest to the formulas' values.
+ * to yq (fq, dense [T][HQ][D]; q NULL: left out), k and v (as it is) into the pages.  What goes into the pages, and yq where fq is a posit, is computed in 64 bits and so the nearest to
+ * the formulas' values; yq in PNN_BF16 and PNN_F32 in 32, as by posit_qk_norm_rope_fwd.  Strides below 2^32 (else PNN_EUNSUPPORTED).
  * A token without a place (before 0, beyond `columns` pages, in a page that is none) is left out of the cache; its query is written all the same.
  * The places of one call's tokens are the caller's to keep apart: of two sequences that share a page both may not write to the same place. */
 int posit_cache_append(void* stream, int fx, int fw, int fq, int fcache, const pnn_paged_desc* desc, const void* q, const void* k, const void* v, const void* wq, const void* wk,

@@ -68,13 +68,16 @@ __device__ __forceinline__ uint32_t f4_power(uint32_t most) {
     e = e < 3 ? 3 : (e > 252 ? 252 : e);
     return most >= 0x7F800000u ? 255u : (uint32_t)e;
 }
-// An element's code: v over the block's power, to nearest, ties to the even code
-__device__ __forceinline__ uint32_t f4_code(float v, float inverse) {
-    const float a = __builtin_fabsf(v) * inverse;
-    const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
-    return c | ((bits_of_f32(v) >> 31) << 3);
-}
 __device__ __forceinline__ float f4_scale(uint32_t power) { return f32_of_bits(power << 23); }
+// Eight elements' codes: over the block's power, to nearest, ties to the even code, 6 for what is above it
+__device__ __forceinline__ uint32_t f4_codes(const float (&v)[8], uint32_t power) {
+    const float s = f4_scale(power);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+}
 // Eight elements of 4 bits
 __device__ __forceinline__ void f4_values(float (&v)[8], uint32_t w, uint32_t power) {
     typedef float v2 __attribute__((ext_vector_type(2)));

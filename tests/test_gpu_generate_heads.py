@@ -45,6 +45,8 @@ def forward(x, w, cos, sin, off, rot, neighbours, eps):
     (4, 3, 1, 22, 10, True, "p16", "p16", "p16"),
     (6, 3, 2, 2, 2, False, "f32", "f32", "f32"),
     (2500, 4, 2, 64, 64, False, "p8_2", "p16", "f32"),   # more rows than workgroups
+    (9001, 1, 1, 24, 16, False, "p8_1", "f32", "bf16"),  # workgroups with more than one block, values from a table
+    (4099, 2, 1, 8, 8, True, "p8", "bf16", "p8"),
 ])
 @pytest.mark.parametrize("how", ["both", "norm", "turn", "none"])
 def test_forward_and_backward(t, hq, hkv, d, rot, neighbours, fx, fw, fy, how):
@@ -59,13 +61,14 @@ def test_forward_and_backward(t, hq, hkv, d, rot, neighbours, fx, fw, fy, how):
     args = dict(positions=gu.dev(pos) if turns else None, inv_freq=freq if turns else None, wq=w[0], wk=w[1], fw=fw, neighbours=neighbours)
     eps = float(np.float32(1e-6))
     yq, yk, rstd = pn.posit_qk_norm_rope_fwd(q, k, fx, fy, eps=1e-6, **args)
-    g = [lu.to_format(lu.normal(rng, v.shape), "bf16") for v in (qv, kv)]
-    dq, dk, dwq, dwk = pn.posit_qk_norm_rope_bwd(g[0], g[1], q, k, rstd, "bf16", fx, fy, fdw="f32", **args)
+    fd = fx if t % 2 and fx != "f32" else "bf16"
+    g = [lu.to_format(lu.normal(rng, v.shape), fd) for v in (qv, kv)]
+    dq, dk, dwq, dwk = pn.posit_qk_norm_rope_bwd(g[0], g[1], q, k, rstd, fd, fx, fy, fdw="f32", **args)
     assert (rstd is None) == (not norm) and (dwq is None) == (dwk is None) == (not norm)
     for n, (x, y, dx, dw, gr) in enumerate(((qv, yq, dq, dwq, g[0]), (kv, yk, dk, dwk, g[1]))):
         want, slack, hat, r = forward(x, wv[n], cos, sin, off, rot, neighbours, eps)
         lu.check(y, want, slack + 1e-37, fy, "y%d" % n)
-        gv = lu.values(gr, "bf16")
+        gv = lu.values(gr, fd)
         gt, gs = (gu.turn(gv, cos, -sin, rot, neighbours), gu.turn_slack(gv, off, rot, neighbours)) if turns else (gv, 0 * gv)
         if not norm:
             lu.check(dx, gt, gs + 1e-37, fy, "dx%d" % n)
