@@ -20,7 +20,7 @@ struct Append {
     ElemFmt fx, fw, fq, fc;
 };
 
-constexpr int APPEND_BLOCK = 4;
+constexpr int APPEND_BLOCK = 8;
 
 // One head's elements: normalised and rotated in T, in the pairs of HeadLane
 template <int L, bool NEIGHBOURS, class T, class T2>
@@ -289,7 +289,7 @@ extern "C" int posit_cache_append(void* stream, int fx, int fw, int fq, int fcac
     a.HQ = (int)d.HQ; a.R = (int)d.R; a.wide = q && is_posit(fq); a.eps = d.eps;
     a.kw = norm ? kind_of(fw) : 0; a.kq = q ? kind_of(fq) : 0;
     a.fx = elem_fmt(fx); a.fw = elem_fmt(norm ? fw : fx); a.fq = elem_fmt(q ? fq : fx); a.fc = elem_fmt(fcache);
-    const int64_t block = d.T / 2048;
+    const int64_t block = d.T / 512;
     a.block = block < 1 ? 1 : (block > APPEND_BLOCK ? APPEND_BLOCK : (int)block);
     int64_t groups = (d.T + a.block - 1) / a.block;
     if (groups > 65536) groups = 65536;
