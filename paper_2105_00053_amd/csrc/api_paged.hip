@@ -29,6 +29,7 @@ inline PagedPlan paged_plan(const pnn_paged_desc& d) {
     const int64_t window = d.window < longest ? d.window : 0, sinks = d.sinks < longest ? d.sinks : longest;  // both small: their sum is
     if (window > 0 && window + d.most + sinks + 64 < keys) keys = window + d.most + sinks + 64;
     const int64_t all = (keys + 31) / 32 + 1, groups = d.B * d.HKV * p.blocks;
+    // three workgroups to a compute unit (64 x 8192 of uneven lengths: 82 us, with two 88; even lengths take 126 with three and 114 with two, but the lengths are not known here)
     int64_t parts = groups > 0 ? (768 + groups - 1) / groups : 1;
     if (parts > all / 4) parts = all / 4;
     if (parts > AT_MOST_PARTS) parts = AT_MOST_PARTS;

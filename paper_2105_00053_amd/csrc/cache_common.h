@@ -57,6 +57,12 @@ __device__ __forceinline__ int64_t cache_page(const CacheShape& s, int b, int co
 __device__ __forceinline__ int cache_unit(const CacheShape& s, bool values, int at, int unit) {
     return values ? (((at >> 2) * (s.D >> 3) + unit) * 4 + (at & 3)) * 8 : at * s.D + unit * 8;
 }
+// Of a value, the unit that a lane of 16 takes in attention, where a head is DB blocks of 32 (`full`: whole ones): the lanes share out 64 elements, or 128, and those behind the head's
+// end, which 32 and 96 elements leave too, take its first unit
+__host__ __device__ constexpr int cache_lane_unit(int DB, bool full, int col, int D) {
+    const int unit = (DB <= 2 ? 4 : 8) * col / 8;
+    return (full && (DB == 2 || DB == 4)) || unit < D / 8 ? unit : 0;
+}
 // Byte, from a page's first, of a block's power
 __device__ __forceinline__ int cache_power(const CacheShape& s, bool values, int at, int block) {
     return s.page * s.D / 2 + (values ? ((at >> 2) * s.blocks + block) * 4 + (at & 3) : at * s.blocks + block);

@@ -17,6 +17,7 @@
 #include "p16_window_arith.h"
 #include "noquire_arith.h"
 #include "loss_ops.h"
+#include "cache_common.h"
 
 using namespace pnn;
 
@@ -734,5 +735,8 @@ int hostcheck_direct_conv_plan(int fmt, int which, const pnn_conv2d_desc* d, int
     PNN_DISPATCH_POSIT(fmt, return host_direct_conv_plan<F>(which, g, with_bias != 0, out))
     return 0;
 }
+
+// Unit of a value's head that a lane takes in attention over pages
+int hostcheck_cache_lane_unit(int DB, int full, int col, int D) { return cache_lane_unit(DB, full != 0, col, D); }
 
 }  // extern "C"

@@ -198,3 +198,14 @@ def test_the_plain_forms_agree_with_each_other():
     codes, powers = gu.f4_encode(ties)
     assert powers[0, 0] == 127 and codes[0, :8].tolist() == [7, 0, 2, 2, 4, 4, 6, 14]
     assert gu.f4_encode(np.full((1, 32), 7.0))[1][0, 0] == 127 and gu.f4_encode(np.full((1, 32), np.nextafter(7.0, 8)))[1][0, 0] == 128
+
+
+@pytest.mark.parametrize("d", range(8, 136, 8))
+def test_lanes_stay_inside_a_head(d):
+    """The lanes that attention reads a value's elements with: between them every unit of eight, and none behind the head's end (the last page ends there)."""
+    from paper_2105_00053_amd import build
+    if not os.path.exists(build.HOSTCHECK):
+        build.build()
+    hc = ctypes.CDLL(build.HOSTCHECK)
+    units = {hc.hostcheck_cache_lane_unit((d + 31) // 32, int(d % 32 == 0), col, d) for col in range(16)}
+    assert units == set(range(d // 8))
