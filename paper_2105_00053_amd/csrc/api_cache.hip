@@ -23,7 +23,7 @@ struct Append {
 constexpr int APPEND_BLOCK = 8;
 
 // One head's elements: normalised and rotated in T, in the pairs of HeadLane
-template <int L, bool NEIGHBOURS, class T, class T2>
+template <int L, bool NEIGHBOURS, bool WHOLE, class T, class T2>
 __device__ __forceinline__ void append_head(T (&x)[8], const float (&v)[8], const Append& a, bool norm, const float (&w)[8], const T2* angles, int lane, int half) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = (T)v[e];
@@ -41,15 +41,17 @@ __device__ __forceinline__ void append_head(T (&x)[8], const float (&v)[8], cons
     if (half) {
         T2 cs[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            cs[i] = angles[4 * lane + i];
-        }
-        heads_turn<NEIGHBOURS, false>(x, cs);
+        for (int i = 0; i < 4; ++i) cs[i] = angles[4 * lane + i];
+        // whole heads without a branch in each lane (the prompts below: 138 us with their reading, 157 with it); lanes behind the head's end turn what nobody stores
+        if (2 * half == a.s.D) heads_turn<NEIGHBOURS, WHOLE, false>(x, cs, 4);
+        else heads_turn<NEIGHBOURS, WHOLE, false>(x, cs, half - 4 * lane);
     }
 }
 
 // A block of rows to a workgroup; 8 or 16 lanes take a head, eight elements to each: of queries and keys four pairs that are rotated, of values and for the cache eight in a row.
 // Queries, keys and values are a pass each; of few rows each pass's rounds go to workgroups of their own (gridDim.y).
+// Bound by the vector unit, 66 % busy: keys in binary64, conversions of queries.  9 prompts of up to 2048 tokens, 32 + 8 heads of 128, posit<8,2> to bfloat16 and 4 bits: 108 to 111 us, where
+// memory would take about 40; 4 tokens 6 us.
 template <int L, int KC, int KX, bool NEIGHBOURS, bool WHOLE>
 __global__ __launch_bounds__(256, 3) void cache_append_kernel(Append a) {
     __shared__ double2 wide[APPEND_BLOCK * 64];
@@ -86,15 +88,13 @@ __global__ __launch_bounds__(256, 3) void cache_append_kernel(Append a) {
         }
         __syncthreads();
         if (half)
-            for (int i = t; i < rows * (D / 2); i += 256) {
-                const int r = i / (D / 2), p = i - r * (D / 2);
-                double sn = 0.0, cs = 1.0;
-                if (p < half && seq[r] >= 0) {
-                    // as turns, of which only the fraction counts
-                    double x = (double)pos[r] * a.freq[p] * 0.15915494309189535;
-                    x -= rint(x);
-                    sincospi(2.0 * x, &sn, &cs);
-                }
+            for (int i = t; i < rows * half; i += 256) {
+                const int r = i / half, p = i - r * half;
+                if (seq[r] < 0) continue;
+                // as turns, of which only the fraction counts
+                double x = (double)pos[r] * a.freq[p] * 0.15915494309189535, sn, cs;
+                x -= rint(x);
+                sincospi(2.0 * x, &sn, &cs);
                 wide[r * 64 + p] = make_double2(cs, sn);
                 narrow[r * 64 + p] = make_float2((float)cs, (float)sn);
             }
@@ -154,10 +154,10 @@ __global__ __launch_bounds__(256, 3) void cache_append_kernel(Append a) {
             pass(0, a.q, a.HQ, [&](int r, int h, float (&v)[8]) {
                 if (a.wide) {
                     double x[8];
-                    append_head<L, NEIGHBOURS>(x, v, a, a.wq != nullptr, w, wide + r * 64, lane, half);
+                    append_head<L, NEIGHBOURS, WHOLE>(x, v, a, a.wq != nullptr, w, wide + r * 64, lane, half);
                     f32_for_rounding(v, x, a.kq == KIND_POSIT_U8 ? ZEROS_8 : ZEROS_16);
                 } else {
-                    append_head<L, NEIGHBOURS>(v, v, a, a.wq != nullptr, w, narrow + r * 64, lane, half);
+                    append_head<L, NEIGHBOURS, WHOLE>(v, v, a, a.wq != nullptr, w, narrow + r * 64, lane, half);
                 }
                 Raw8 raw;
                 raw8<false>(raw, v, a.kq, a.fq);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(256, 3) void cache_append_kernel(Append a) {
         pass(1, a.k, s.HKV, [&](int r, int h, float (&v)[8]) {
             if (a.wk || half) {
                 double x[8];
-                append_head<L, NEIGHBOURS>(x, v, a, a.wk != nullptr, w, wide + r * 64, lane, half);
+                append_head<L, NEIGHBOURS, WHOLE>(x, v, a, a.wk != nullptr, w, wide + r * 64, lane, half);
                 f32_for_rounding(v, x, ZEROS_8);
             }
             // from pairs to rows, inside the wave
@@ -203,7 +203,7 @@ struct CacheRead {
     ElemFmt fc, fout;
 };
 
-// Four tokens' eight elements to a thread, of keys or (blockIdx.y) values: a value's four lie side by side.
+// Four tokens' eight elements to a thread, of keys or (blockIdx.y) values: a value's four lie side by side.  Bound by the stores: the cache of the prompts above to bfloat16 in 20 us.
 template <int KC>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRead a) {
     const CacheShape& s = a.s;

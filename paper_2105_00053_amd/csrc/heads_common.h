@@ -160,17 +160,23 @@ __device__ __forceinline__ void heads_store(const Raw8& r, const HeadLane<NEIGHB
     }
 }
 
-// The lane's pairs by its angles; BACK: by their negatives
-template <bool NEIGHBOURS, bool BACK, class T, class T2>
-__device__ __forceinline__ void heads_turn(T (&v)[8], const T2 (&cs)[4]) {
+// The lane's first n pairs by their angles, the others as they are (an infinity there would make a NaN of its partner); BACK: by the negatives.  A lane of WHOLE halves has all of its
+// pairs before R or none.
+template <bool NEIGHBOURS, bool WHOLE, bool BACK, class T, class T2>
+__device__ __forceinline__ void heads_turn(T (&v)[8], const T2 (&cs)[4], int n) {
+    constexpr int step = NEIGHBOURS ? 2 : 1, gap = NEIGHBOURS ? 1 : 4;
+    auto turn = [&](auto all) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        constexpr int step = NEIGHBOURS ? 2 : 1, gap = NEIGHBOURS ? 1 : 4;
-        const int x = step * i, y = x + gap;
-        const T s = BACK ? -cs[i].y : cs[i].y, a = v[x], b = v[y];
-        v[x] = __builtin_elementwise_fma(a, cs[i].x, -(b * s));
-        v[y] = __builtin_elementwise_fma(b, cs[i].x, a * s);
-    }
+        for (int i = 0; i < 4; ++i) {
+            const int x = step * i, y = x + gap;
+            const T s = BACK ? -cs[i].y : cs[i].y, a = v[x], b = v[y];
+            const T ta = __builtin_elementwise_fma(a, cs[i].x, -(b * s)), tb = __builtin_elementwise_fma(b, cs[i].x, a * s);
+            v[x] = all() || i < n ? ta : a;
+            v[y] = all() || i < n ? tb : b;
+        }
+    };
+    if (n >= 4) turn([] { return true; });
+    else if ((!WHOLE || NEIGHBOURS) && n > 0) turn([] { return false; });
 }
 
 // Values of 8-bit posits by look-up: 16 copies of each in LDS, so that the lanes of a wave meet few conflicts (three instructions an element where decoding takes 13)

@@ -164,3 +164,27 @@ def test_gradients_by_differences(neighbours):
         e = np.zeros(d)
         e[i] = step
         assert abs((total(x, w + e) - total(x, w - e)) / (2 * step) - dw[i].item()) < 0.01
+
+
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("d, rot", [(48, 16), (48, 36), (50, 18)])
+def test_what_is_not_rotated_stays(d, rot, neighbours):
+    """Elements from `rot` on are the given ones, whatever stands beside them: infinities and NaN reach no other element there, and no rotated one."""
+    rng = np.random.default_rng(d + rot)
+    x = lu.normal(rng, (9, 4, d))
+    x[2, 1, rot:] = np.where(np.arange(d - rot) % 3 == 0, np.inf, x[2, 1, rot:])
+    x[5, 3, d - 1], x[6, 0, rot + 1] = np.nan, -np.inf
+    t, pos, freq = lu.to_format(x, "f32"), torch.arange(3, 12, dtype=torch.int32, device="cuda"), pn.rope_frequencies(rot)
+    how = dict(positions=pos, inv_freq=freq, neighbours=neighbours)
+    outs = list(pn.posit_qk_norm_rope_fwd(t[:, :3], t[:, 3:], "f32", "f32", **how)[:2])
+    outs += pn.posit_qk_norm_rope_bwd(t[:, :3], t[:, 3:], t[:, :3], t[:, 3:], None, "f32", "f32", "f32", **how)[:2]
+    got = [torch.cat(outs[:2], 1), torch.cat(outs[2:], 1)]
+    if d % 8 == 0:
+        k, v = pn.posit_cache_pages(1, 4, 16, d, "bf16")
+        table, lens, starts = gu.dev(np.array([[0]], np.int32)), gu.dev(np.array([12], np.int32)), gu.dev(np.array([0, 9], np.int32))
+        got.append(pn.posit_cache_append(t, t, k, v, table, lens, "f32", "bf16", starts=starts, q=t, fq="f32", inv_freq=freq, neighbours=neighbours))
+        dense = pn.posit_cache_read(k, v, table, lens, 12, d, "bf16", "f32")[0][0, 3:]
+        want = lu.values(lu.to_format(x, "bf16"), "bf16")
+        assert np.array_equal(dense[..., rot:].cpu().numpy(), want[..., rot:], equal_nan=True) and torch.isfinite(dense[..., :rot]).all()
+    for y in got:
+        assert np.array_equal(y[..., rot:].cpu().numpy(), x[..., rot:], equal_nan=True) and torch.isfinite(y[..., :rot]).all()
