@@ -138,6 +138,7 @@ struct SampleWeight {
 // NC: vectors of eight logits that a thread holds in registers, so that memory is read once; 0: rows of any length, read again by each pass.
 // SAMPLE_WHOLE: a row to a workgroup.  Few long rows would leave most of the chip without work, so they go in parts of 8 NC logits a thread: SAMPLE_TOPS finds the parts' largest, SAMPLE_PARTS
 // counts and weighs them into the rows' first bins (sums of integers, the same in any order), SAMPLE_JOIN does the rest, a row to a workgroup.
+// Bound by the weights in binary64 and the search's passes: 256 x 50021 posit<16,1>, all limits: loads and maximum 4 us, weights into the histogram 20, the three places 20; memory would take 5.
 enum SamplePhase { SAMPLE_WHOLE, SAMPLE_TOPS, SAMPLE_PARTS, SAMPLE_JOIN };
 
 template <int K, int NC, int PHASE>
@@ -603,9 +604,8 @@ inline int sample_shift(int64_t vocab) {
     return 62 - bits < 51 ? 62 - bits : 51;
 }
 
-// Logits of a part, 0: rows are taken whole.
-inline int64_t sample_part(int fz, int64_t rows, int64_t vocab) {
-    (void)fz;
+// Logits of a part, 0: rows are taken whole.  Parts pay where rows leave compute units idle (1 x 100003: 36 to 40 us), not where there are two rows to a compute unit anyhow (256 x 50021: 50 whole).
+inline int64_t sample_part(int64_t rows, int64_t vocab) {
     return rows <= 128 && vocab > 16384 ? SAMPLE_THREADS * 8 : 0;
 }
 
@@ -635,7 +635,7 @@ using namespace pnn;
 
 extern "C" size_t posit_sample_workspace(int fz, int64_t rows, int64_t vocab) {
     if (element_status(fz) || rows <= 0 || vocab <= 0 || rows >= ((int64_t)1 << 31) || vocab >= ((int64_t)1 << 31)) return 0;
-    const int64_t part = sample_part(fz, rows, vocab);
+    const int64_t part = sample_part(rows, vocab);
     if (part == 0) return 0;
     return (size_t)rows * (SAMPLE_BINS * 8 + (SAMPLE_BINS + 1 + (vocab + part - 1) / part) * 4);
 }
@@ -653,7 +653,7 @@ extern "C" int posit_sample(void* stream, int fz, int64_t rows, int64_t vocab, c
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
     Sample a = {logits, u, temperature, top_p, min_p, top_k, token, kept, logprob, vocab, ldz, sample_shift(vocab), elem_fmt(fz), 0, 0, nullptr, nullptr, nullptr};
-    if (const int64_t part = sample_part(fz, rows, vocab)) {
+    if (const int64_t part = sample_part(rows, vocab)) {
         a.parts = (int)((vocab + part - 1) / part);
         a.weights = (unsigned long long*)workspace;
         a.counts = (uint32_t*)(a.weights + rows * SAMPLE_BINS);
