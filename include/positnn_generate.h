@@ -78,7 +78,7 @@ int posit_cache_append(void* stream, int fx, int fw, int fq, int fcache, const p
                        const double* inv_freq, const int32_t* starts, const int32_t* lens, const int32_t* table, void* k_pages, void* v_pages, void* yq);
 
 /* The cache's values as dense rows k, v [B][longest][HKV][D] in fout: what posit_attention_fwd takes for a prompt on a filled cache.  Zeros behind a
- * sequence's end. */
+ * sequence's end; NaN for tokens that lens counts beyond `columns` pages. */
 int posit_cache_read(void* stream, int fcache, int fout, const pnn_paged_desc* desc, const int32_t* lens, const int32_t* table, const void* k_pages, const void* v_pages, void* k, void* v);
 
 /* Attention of the packed rows q (fq, a format that bfloat16 holds exactly; strides ql, qh) over the pages, as posit_attention_fwd: row t of sequence b, at position

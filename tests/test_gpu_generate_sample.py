@@ -72,7 +72,7 @@ def test_equal_logits_are_drawn_by_their_indices():
     n = 4096
     u = np.array([0, 0.25, 0.5, 0.75, 1 / 4096, 1 / 4096 - 2.0 ** -30, ONE], np.float32)
     (token, logprob, kept), _ = run(np.zeros((7, n), np.float32), "f32", u)
-    assert token.tolist() == [0, 1024, 2048, 3072, 1, 0, 4095] and (kept == n).all()
+    assert token.tolist() == [0, 1024, 2048, 3 * 1024, 1, 0, 4095] and (kept == n).all()
     assert np.allclose(logprob, -np.log(n), rtol=1e-7)
     for k, p, want in ((3, 1.0, 3), (0, 0.5, 2048), (0, 0.50001, 2049), (100, 0.25, 25), (1, 0.0, 1), (0, 0.0, 1), (0, -1.0, 1), (0, np.nan, n)):
         (_, _, kept), _ = run(np.zeros((1, n), np.float32), "f32", [0.0], top_k=k, top_p=p)
