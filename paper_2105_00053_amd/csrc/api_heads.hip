@@ -15,7 +15,7 @@ struct Heads {
     const double* freq;
     uint32_t xl[2], xh[2], gl[2], gh[2];
     int T, H[2], D, R, block;        // block: rows that share a workgroup's angles
-    int table;                       // 8-bit posits through a table: 1 of x, 2 of the gradients too, which have x's format
+    int table;                       // 8-bit posits through a table (forward and backward of 7 rows 19.7 us and 20.3 without, of 4096 51 and 72): 1 of x, 2 of the gradients too, which have x's format
     float eps;
     int kg, kw, ky, kdw;
     ElemFmt fx, fg, fw, fy, fdw;
@@ -251,9 +251,6 @@ inline HeadsPlan heads_plan(const pnn_heads_desc& d, int64_t most) {
     return p;
 }
 
-// A table of values pays where a workgroup has two blocks or more to look up; of one block, building it takes as long as decoding
-inline int heads_look(int fx, const HeadsPlan& p, const pnn_heads_desc& d) { return kind_of(fx) == KIND_POSIT_U8 && d.T >= p.groups * 2; }
-
 inline int heads_status(const pnn_heads_desc* d, bool back) {
     if (!d || d->T < 0 || d->HQ < 0 || d->HKV < 0 || d->D < 0 || d->R < 0 || d->R > d->D || d->R % 2 != 0 || !(d->eps >= 0.f)) return PNN_EINVAL;
     if (d->ql < 0 || d->qh < 0 || d->kl < 0 || d->kh < 0) return PNN_EINVAL;
@@ -310,7 +307,7 @@ extern "C" int posit_qk_norm_rope_fwd(void* stream, int fx, int fw, int fy, cons
     a.pos = pos; a.freq = inv_freq;
     a.xl[0] = (uint32_t)d.ql; a.xl[1] = (uint32_t)d.kl; a.xh[0] = (uint32_t)d.qh; a.xh[1] = (uint32_t)d.kh;
     a.T = (int)d.T; a.H[0] = (int)d.HQ; a.H[1] = (int)d.HKV; a.D = (int)d.D; a.R = (int)d.R; a.block = p.block; a.eps = d.eps;
-    a.kw = norm ? kind_of(fw) : 0; a.ky = kind_of(fy); a.table = heads_look(fx, p, d);
+    a.kw = norm ? kind_of(fw) : 0; a.ky = kind_of(fy); a.table = kind_of(fx) == KIND_POSIT_U8;
     a.fx = elem_fmt(fx); a.fw = elem_fmt(norm ? fw : fx); a.fy = elem_fmt(fy);
     PNN_DISPATCH_KIND(kind_of(fx), (launch_heads<false, K>((hipStream_t)stream, p, d.neighbours != 0, a)))
     return hip_status(hipGetLastError());
@@ -347,7 +344,7 @@ extern "C" int posit_qk_norm_rope_bwd(void* stream, int fd, int fx, int fw, int 
     a.T = (int)d.T; a.H[0] = (int)d.HQ; a.H[1] = (int)d.HKV; a.D = (int)d.D; a.R = (int)d.R; a.block = p.block; a.eps = d.eps;
     a.kg = kind_of(fd); a.kw = norm ? kind_of(fw) : 0; a.ky = kind_of(fdx); a.kdw = want ? kind_of(fdw) : 0;
     a.fx = elem_fmt(fx); a.fg = elem_fmt(fd); a.fw = elem_fmt(norm ? fw : fx); a.fy = elem_fmt(fdx); a.fdw = elem_fmt(want ? fdw : fx);
-    a.table = heads_look(fx, p, d) ? (fd == fx ? 2 : 1) : 0;
+    a.table = kind_of(fx) == KIND_POSIT_U8 ? (fd == fx ? 2 : 1) : 0;
     a.part = want ? (float*)workspace : nullptr;
     hipStream_t st = (hipStream_t)stream;
     PNN_DISPATCH_KIND(kind_of(fx), (launch_heads<true, K>(st, p, d.neighbours != 0, a)))

@@ -604,10 +604,9 @@ inline int sample_shift(int64_t vocab) {
     return 62 - bits < 51 ? 62 - bits : 51;
 }
 
-// Logits of a part, 0: rows are taken whole.  Parts pay where rows leave compute units idle (1 x 100003: 36 to 40 us), not where there are two rows to a compute unit anyhow (256 x 50021: 50 whole).
-inline int64_t sample_part(int64_t rows, int64_t vocab) {
-    return rows <= 128 && vocab > 16384 ? SAMPLE_THREADS * 8 : 0;
-}
+// Logits of a part, 0: rows are taken whole.  Parts pay where rows are long and few, even is about 1 x 30000, and the few us lost below it are left (posit<16,1>, all limits, us whole and in parts: 1 x 20011 27 and 31, 1 x 50021 40 and 34,
+// 32 x 50021 47 and 44, 128 x 50021 50 and 62, 1 x 100003 66 and 43, 64 x 100003 85 and 78, 128 x 100003 89 and 96).
+inline int64_t sample_part(int64_t rows, int64_t vocab) { return vocab > 16384 && rows <= vocab / 1024 ? SAMPLE_THREADS * 8 : 0; }
 
 // Rows that fit the threads' registers, 32 words each, stay there.
 template <int K>
