@@ -6,6 +6,7 @@
 // is the same in any order and the result does not depend on the device's.
 #include "../../include/positnn_generate.h"
 #include "lm_codec.h"
+#include "sample_bins.h"
 
 namespace pnn {
 
@@ -26,7 +27,7 @@ struct Sample {
     unsigned long long* weights; // [row][bins]
 };
 
-constexpr int SAMPLE_THREADS = 1024, SAMPLE_BITS = 11, SAMPLE_BINS = 1 << SAMPLE_BITS, SAMPLE_LIST = 512, SAMPLE_COPIES = 16;
+constexpr int SAMPLE_THREADS = 1024, SAMPLE_LIST = 512, SAMPLE_COPIES = 16;
 
 struct SampleBins {
     uint32_t count[SAMPLE_BINS];     // sums from the first bin to each, behind sample_sums
@@ -245,6 +246,10 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
     top = wave_max_u32(top);
     if ((t & 63) == 0) part[t >> 6] = top;
     if (t < 256) sh.powers[t] = exp2((double)t * (1.0 / 256));
+    if (t == 0) {
+        sh.found = sh.found_weight = sh.found_own = 0;
+        sh.found_before = 0;
+    }
     sample_clear(sh.first);
     if (K == KIND_POSIT_U8) sample_clear(sh.next);  // the copies
     bad = __syncthreads_or(bad);
@@ -282,9 +287,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
     const double likely_from = (double)least * unit < 0.25 ? 0.0 : (double)least * unit;
     uint32_t likely = 0;  // of at least min_p
     // The first bins: of posits a key's highest bits, of floats the difference to the largest in steps of 1/2048 of the range whose weights are not nothing (a float's highest bits would
-    // leave thousands in a bin)
-    const float mf = (float)m, scale = greedy ? 0.f : fminf((float)(2047.0 * inverse / ((a.shift + 3) * 0.6931471805599453)), 1e38f);
-    auto bin_of = [&](uint32_t key, float v) -> int { return POSIT ? (int)((key ^ ((1u << KEY % 32) - 1u)) >> DOWN) : (int)fminf((mf - v) * scale, 2047.f); };
+    // leave thousands in a bin); -inf is in none
+    const float mf = (float)m, scale = sample_bin_scale(a.shift, inverse, greedy);
+    auto bin_of = [&](uint32_t key, float v) -> int { return POSIT ? (int)((key ^ ((1u << KEY % 32) - 1u)) >> DOWN) : sample_float_bin(v, mf, scale); };
     if (PHASE == SAMPLE_JOIN) {
         for (int i = t; i < SAMPLE_BINS; i += SAMPLE_THREADS) {
             sh.first.count[i] = a.counts[row * (SAMPLE_BINS + 1) + i];
@@ -312,11 +317,9 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
         const bool some = a.min_p != nullptr;
         auto add = [&](uint32_t x, float v) {
             // -inf is not counted: most of a row may be, and all of it in one bin
-            const uint32_t k = key_of(x);
             const double e = weight.raw(v);
-            const int bin = bin_of(k, v);
-            const bool in = POSIT || k > NONE;
-            if (in) {
+            const int bin = bin_of(POSIT ? key_of(x) : 0u, v);
+            if (POSIT || bin >= 0) {
                 atomicAdd(&sh.first.count[bin], 1u);
                 atomicAdd(&sh.first.weight[bin], SampleWeight::whole(e));
                 if (some) likely += e >= likely_from ? 1 : 0;
@@ -369,7 +372,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
     const uint32_t all = sh.first.count[SAMPLE_BINS - 1];
     if (!a.min_p) likely = all;
 
-    // vectors with a logit in the first bins' `bin`: which of those in registers have one first, then one after the other, so that what is done with them stands here once
+    // vectors with a logit in the first bins' `bin`, so no more of them than logits that it counts: which of those in registers have one first, then one after the other, so that what is done with them stands here once
     auto has = [&](const Eight& r, int bin) -> bool {
         if (K == KIND_POSIT_U16) {
             // the patterns' bits in the place of the key's, two in a word: whether one is zero
@@ -416,7 +419,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
             }
         }
     };
-    auto in_bin = [&](uint32_t k, int bin) { return k > NONE && bin_of(k, POSIT ? 0.f : value_of_key(k)) == bin; };
+    auto in_bin = [&](uint32_t k, int bin) { return bin_of(k, POSIT ? 0.f : value_of_key(k)) == bin; };
     auto each_of = [&](const Eight& r, int left, int bin, auto f) {
 #pragma nounroll
         for (int e = 0; e < 8 && e < left; ++e) {
@@ -442,7 +445,7 @@ __global__ __launch_bounds__(SAMPLE_THREADS) void sample_kernel(Sample a) {
             return p;
         }
         if (p.n <= (uint32_t)SAMPLE_LIST) {
-            // few logits: each finds its place among them
+            // few logits: each finds its place among them, one of them the place that is looked for.  The list holds their vectors, too: each has one of the bin's logits at least.
             if (listed != bin) {
                 __syncthreads();
                 if (t == 0) sh.listed = sh.runs = 0;

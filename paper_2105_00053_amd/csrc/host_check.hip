@@ -18,6 +18,7 @@
 #include "noquire_arith.h"
 #include "loss_ops.h"
 #include "cache_common.h"
+#include "sample_bins.h"
 
 using namespace pnn;
 
@@ -738,5 +739,11 @@ int hostcheck_direct_conv_plan(int fmt, int which, const pnn_conv2d_desc* d, int
 
 // Unit of a value's head that a lane takes in attention over pages
 int hostcheck_cache_lane_unit(int DB, int full, int col, int D) { return cache_lane_unit(DB, full != 0, col, D); }
+
+// First bins of the draw, of n floats
+void hostcheck_sample_bins(int shift, double inverse, int greedy, float top, const float* v, int n, int* bins) {
+    const float scale = sample_bin_scale(shift, inverse, greedy != 0);
+    for (int i = 0; i < n; ++i) bins[i] = sample_float_bin(v[i], top, scale);
+}
 
 }  // extern "C"
