@@ -45,7 +45,8 @@ int posit_qk_norm_rope_fwd(void* stream, int fx, int fw, int fy, const pnn_heads
 
 /* Gradients for dyq and dyk (fd): with g the gradient rotated back (by -angle) and xhat = x * rstd
  *   dx = round_fdx( rstd * (g * w - xhat * mean(g * w * xhat)) ),  dw = round_fdw( sum over rows and heads of g * xhat )
- * (without norm dx = g).  rstd is that of the forward call (NULL without norm).  dq and dk are dense; dwq and dwk may be NULL. */
+ * (without norm dx = g).  rstd is that of the forward call (NULL without norm).  dq and dk are dense; dwq and dwk may be NULL, and are zeros where queries or keys alone have no
+ * heads. */
 int posit_qk_norm_rope_bwd(void* stream, int fd, int fx, int fw, int fdx, int fdw, const pnn_heads_desc* desc, const void* dyq, const void* dyk, const void* q,
                            const void* k, const void* wq, const void* wk, const float* rstd, const int32_t* pos, const double* inv_freq, void* dq, void* dk, void* dwq,
                            void* dwk, void* workspace, size_t workspace_bytes);

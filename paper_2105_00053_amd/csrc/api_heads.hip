@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256, 4) void heads_bwd_kernel(Heads a) {
         }
     }
     if (!a.part) return;
-    // the groups' sums, in their order, to the workgroup's row
+    // the groups' sums, in their order, to the workgroup's row (zeros for queries or keys that have no heads)
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
@@ -336,7 +336,7 @@ extern "C" int posit_qk_norm_rope_bwd(void* stream, int fd, int fx, int fw, int 
     discard_stale_hip_error();
     const HeadsPlan p = heads_plan(d, HEADS_GROUPS);
     Heads a = {};
-    a.x[0] = q; a.x[1] = k; a.g[0] = dyq; a.g[1] = dyk; a.y[0] = dq; a.y[1] = dk; a.dw[0] = d.HQ > 0 ? dwq : nullptr; a.dw[1] = d.HKV > 0 ? dwk : nullptr; a.rstd = rstd;
+    a.x[0] = q; a.x[1] = k; a.g[0] = dyq; a.g[1] = dyk; a.y[0] = dq; a.y[1] = dk; a.dw[0] = dwq; a.dw[1] = dwk; a.rstd = rstd;
     a.w[0] = norm ? (wq ? wq : wk) : nullptr; a.w[1] = wk;
     a.pos = pos; a.freq = inv_freq;
     a.xl[0] = (uint32_t)d.ql; a.xl[1] = (uint32_t)d.kl; a.xh[0] = (uint32_t)d.qh; a.xh[1] = (uint32_t)d.kh;

@@ -97,7 +97,7 @@ PyObject* heads_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const long dev = a.i[1], fd = a.i[2], fx = a.i[3], fw = a.i[4], fdx = a.i[5], fdw = a.i[6];
         GenHeads g;
         const at::Tensor *gq, *gk = nullptr, *rstd;
-        if (!lm_format(fdx) || !lm_format(fdw) || !gen_heads_args(a.o + 2, fx, fw, dev, &g) || g.d.T == 0) return none();
+        if (!lm_format(fdx) || !lm_format(fdw) || !gen_heads_args(a.o + 2, fx, fw, dev, &g) || g.d.T == 0 || g.d.HQ + g.d.HKV == 0) return none();
         if (!gen_heads(a.o[0], fd, dev, &gq) || gq->sizes() != g.q->sizes()) return none();
         if (g.k && (!gen_heads(a.o[1], fd, dev, &gk) || gk->sizes() != g.k->sizes())) return none();
         if (!gen_vector(a.o[8], at::kFloat, g.d.T * (g.d.HQ + g.d.HKV), dev, &rstd) || !rstd != !g.wq) return none();

@@ -164,7 +164,7 @@ def posit_qk_norm_rope_bwd(dyq, dyk, q, k, rstd, fd, fx, fdx, positions=None, in
     dev, want = q.device, want_dw and wq is not None
     dq = torch.empty(q.shape, dtype=_dtype(fdx), device=dev)
     dk = None if k is None else torch.empty(k.shape, dtype=_dtype(fdx), device=dev)
-    make = torch.zeros if desc.T == 0 else torch.empty
+    make = torch.zeros if desc.T == 0 or desc.HQ + desc.HKV == 0 else torch.empty  # sums over nothing
     dwq = make((desc.D,), dtype=_dtype(fdw), device=dev) if want else None
     dwk = make((desc.D,), dtype=_dtype(fdw), device=dev) if want and k is not None else None
     L = _load()
