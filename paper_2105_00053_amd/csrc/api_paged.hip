@@ -90,7 +90,7 @@ extern "C" int posit_attention_paged(void* stream, int fq, int fcache, int fout,
     AttnPaged a = {};
     a.s = cache_shape(d, fcache, starts, lens, table);
     const int64_t keys = paged_keys(d);
-    a.n.LK = (int)(d.pages > 0 ? keys : 0);
+    a.n.LK = (int)keys;
     a.n.window = d.window >= keys ? 0 : (int)d.window;  // a window of all keys is none
     a.n.sinks = (int)(d.sinks < keys ? d.sinks : keys);
     a.n.HKV = (int)d.HKV; a.n.G = (int)(d.HQ / d.HKV); a.n.D = (int)d.D; a.n.scale = d.scale;
@@ -99,6 +99,10 @@ extern "C" int posit_attention_paged(void* stream, int fq, int fcache, int fout,
     a.rows = p.rows; a.blocks = p.blocks; a.tiles = p.tiles; a.parts = p.parts; a.part = (float*)workspace;
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
+    if (d.pages == 0) {
+        hipLaunchKernelGGL(attn_paged_none_kernel, dim3((unsigned)d.most, (unsigned)d.B), dim3(256), 0, st, a);
+        return hip_status(hipGetLastError());
+    }
     const dim3 grid((unsigned)((int64_t)p.blocks * p.parts * d.HKV * d.B));
     switch (cache_kind(fcache)) {
         case CACHE_U8: launch_paged<CACHE_U8>(st, grid, a); break;

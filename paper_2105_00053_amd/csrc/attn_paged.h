@@ -568,4 +568,17 @@ __global__ __launch_bounds__(512) void attn_paged_join_kernel(AttnPaged a) {
     store_value(a.o, to * D + t, a.ko, a.fo, o);
 }
 
+// A cache without pages, which has nothing to read: every token lies in a page that is none, so a row that sees one is NaN.  A new row to a workgroup.
+__global__ __launch_bounds__(256) void attn_paged_none_kernel(AttnPaged a) {
+    const int i = blockIdx.x, b = blockIdx.y;
+    const PagedRows x(a, b);
+    if (i >= x.count) return;
+    const bool sees = x.base + i >= 0;  // itself
+    const int heads = a.n.HKV * a.n.G;
+    const int64_t row = x.first + i;
+    for (int64_t e = threadIdx.x; e < (int64_t)heads * a.n.D; e += 256) store_value(a.o, row * heads * a.n.D + e, a.ko, a.fo, f32_of_bits(sees ? 0x7FC00000u : 0u));
+    if (a.lse)
+        for (int h = threadIdx.x; h < heads; h += 256) a.lse[row * heads + h] = f32_of_bits(sees ? 0x7FC00000u : 0xFF800000u);
+}
+
 }  // namespace pnn
