@@ -168,20 +168,34 @@ class PagedDecoder:
 
     def step(self, new, most_rows=64):
         """Logits behind the last new token of each sequence, in the order of new = {name: its tokens, a list of one or more}; sequences that are not known begin.  Rows that share a key head with
-        at most `most_rows` others of their sequence read the pages themselves; where there are more, as for prompts, the pages are read back and go through posit_attention_fwd."""
+        at most `most_rows` others of their sequence read the pages themselves; where there are more, as for prompts, the pages are read back and go through posit_attention_fwd.  A step that is
+        refused leaves the sequences and the free pages as they were."""
+        logits, *after = self._run(new, most_rows)
+        self._take(*after)
+        return logits
+
+    def _take(self, held, left):
+        """What a step leaves: its sequences' pages and tokens, and how many of the free pages."""
+        self.held.update(held)
+        del self.free[left:]
+
+    def _run(self, new, most_rows=64):
+        """(logits, and what _take makes of the state behind them); the state stays."""
         net, fc, dev = self.net, self.net.compute, self.net.table.device
         if not new or not all(len(tokens) for tokens in new.values()):
             raise pn.PositError("a step takes one token or more of each of its sequences")
         need = {name: -(-(self.length(name) + len(tokens)) // self.page) - len(self.held.get(name, ((), 0))[0]) for name, tokens in new.items()}
         if sum(need.values()) > len(self.free):
             raise pn.PositError("%d pages are free, the step takes %d" % (len(self.free), sum(need.values())))
+        held, left = {}, len(self.free)
         for name, tokens in new.items():
             pages, n = self.held.get(name, ([], 0))
-            self.held[name] = (pages + [self.free.pop() for _ in range(need[name])], n + len(tokens))
+            held[name] = (pages + self.free[left - need[name]:left][::-1], n + len(tokens))
+            left -= need[name]
         names, counts = list(new), [len(tokens) for tokens in new.values()]
-        columns, longest, most = max(len(self.held[name][0]) for name in names), max(self.length(name) for name in names), max(counts)
+        columns, longest, most = max(len(held[name][0]) for name in names), max(held[name][1] for name in names), max(counts)
         # one copy to the device: the table, lengths, first rows and tokens side by side
-        flat = [p for name in names for p in self.held[name][0] + [-1] * (columns - len(self.held[name][0]))] + [self.length(name) for name in names]
+        flat = [p for name in names for p in held[name][0] + [-1] * (columns - len(held[name][0]))] + [held[name][1] for name in names]
         starts = [0]
         for c in counts:
             starts.append(starts[-1] + c)
@@ -206,8 +220,11 @@ class PagedDecoder:
             o = _movable(o).view(b * most, net.heads, net.d)[at]
         last = (starts[1:] - 1).long()
         _, _, _, logits = _read_out(net, x[last], _movable(o.reshape(len(tokens), -1))[last])
-        return logits
+        return logits, held, left
 
     def sample(self, new, u, **limits):
         """(token, logprob, kept) of the draw behind each sequence's new tokens, in the order of `new`: u and the limits as posit_sample takes them."""
-        return generate.posit_sample(self.step(new), u, self.net.loss, **limits)
+        logits, *after = self._run(new)
+        drawn = generate.posit_sample(logits, u, self.net.loss, **limits)
+        self._take(*after)
+        return drawn
