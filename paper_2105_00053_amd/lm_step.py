@@ -184,6 +184,10 @@ class PagedDecoder:
         net, fc, dev = self.net, self.net.compute, self.net.table.device
         if not new or not all(len(tokens) for tokens in new.values()):
             raise pn.PositError("a step takes one token or more of each of its sequences")
+        # an index beyond the table would end the process on the device, and -1, which a draw without candidates gives, would be its last row
+        vocab = net.table.shape[0]
+        if any(min(tokens) < 0 or max(tokens) >= vocab for tokens in new.values()):
+            raise pn.PositError("a token is none of the table's %d" % vocab)
         need = {name: -(-(self.length(name) + len(tokens)) // self.page) - len(self.held.get(name, ((), 0))[0]) for name, tokens in new.items()}
         if sum(need.values()) > len(self.free):
             raise pn.PositError("%d pages are free, the step takes %d" % (len(self.free), sum(need.values())))
