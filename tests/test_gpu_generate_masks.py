@@ -57,3 +57,20 @@ def test_the_same_every_time(fmt):
     assert first[2].tolist() == [20] * 3
     for _ in range(20):
         assert all(torch.equal(a, b) for a, b in zip(first, pn.posit_sample(t, torch.from_numpy(u).cuda(), fmt, **how)))
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,vocab", [(6, 9001), (6, 40003), (6, 700), (2, 70001)])
+def test_ends_of_the_temperatures_over_a_mask(fmt, rows, vocab):
+    """The likeliest alone, shares alike, all weight on one: bins of no width, one bin for all, and nearly all in the last."""
+    rng = np.random.default_rng(rows * vocab)
+    for allowed in (1, 40, 650):
+        z = masked(rng, rows, vocab, allowed, 30.0)
+        z[0, z[0] > -np.inf] = 2.5                                    # equal ones
+        z[1, rng.choice(np.flatnonzero(z[1] > -np.inf), 1)] = 3e38    # differences that are infinite, or nearly
+        z[1, rng.choice(np.flatnonzero(z[1] > -np.inf), 1)] = -3e38
+        u = rng.random(rows).astype(np.float32)
+        for temperature in (0.0, np.inf, 1e30, 1e-30, 1e-42):
+            check(z, fmt, u, temperature=temperature)
+            check(z, fmt, u, temperature=temperature, top_k=allowed // 2 + 1)
+            check(z, fmt, u, temperature=temperature, top_k=allowed - allowed // 4, top_p=0.7, min_p=0.2)
