@@ -607,9 +607,15 @@ inline int sample_shift(int64_t vocab) {
     return 62 - bits < 51 ? 62 - bits : 51;
 }
 
-// Logits of a part, 0: rows are taken whole.  Parts pay where rows are long and few, even is about 1 x 30000, and the few us lost below it are left (posit<16,1>, all limits, us whole and in parts: 1 x 20011 27 and 31, 1 x 50021 40 and 34,
-// 32 x 50021 47 and 44, 128 x 50021 50 and 62, 1 x 100003 66 and 43, 64 x 100003 85 and 78, 128 x 100003 89 and 96).
-inline int64_t sample_part(int64_t rows, int64_t vocab) { return vocab > 16384 && rows <= vocab / 1024 ? SAMPLE_THREADS * 8 : 0; }
+// Logits of a part, 0: rows are taken whole.  Parts pay where rows are long and few: they spread the weights over the chip, for two launches more.  All limits, us whole and in parts:
+// posit<16,1>: 1 x 20011 27 and 30, 1 x 32003 33 and 33, 1 x 50021 40 and 34, 32 x 50021 47 and 44, 128 x 50021 50 and 62, 1 x 131072 79 and 46, 64 x 100003 85 and 78, 128 x 131072 98 and 106; binary32:
+// 1 x 20011 26 and 30, 1 x 32003 33 and 33, 8 x 20011 61 and 60, 1 x 50021 48 and 38, 32 x 50021 276 and 209; bfloat16 between these.  So the 3 to 4 us of a single row of less than 32000 are lost.
+// 8-bit posits are counted without weights, and whole is the faster as long as a row fits the registers: 1 x 20011 29 and 36, 32 x 50021 43 and 49, 1 x 131072 40 and 40, 64 x 100003 65 and 77; behind that
+// 1 x 150001 53 and 47, 8 x 200003 89 and 80, 64 x 150001 100 and 108, 128 x 300007 173 and 212.
+inline int64_t sample_part(int fz, int64_t rows, int64_t vocab) {
+    const bool counted = kind_of(fz) == KIND_POSIT_U8;
+    return vocab > (counted ? 131072 : 16384) && rows <= vocab / (counted ? 8192 : 1024) ? SAMPLE_THREADS * 8 : 0;
+}
 
 // Rows that fit the threads' registers, 32 words each, stay there.
 template <int K>
@@ -637,7 +643,7 @@ using namespace pnn;
 
 extern "C" size_t posit_sample_workspace(int fz, int64_t rows, int64_t vocab) {
     if (element_status(fz) || rows <= 0 || vocab <= 0 || rows >= ((int64_t)1 << 31) || vocab >= ((int64_t)1 << 31)) return 0;
-    const int64_t part = sample_part(rows, vocab);
+    const int64_t part = sample_part(fz, rows, vocab);
     if (part == 0) return 0;
     return (size_t)rows * (SAMPLE_BINS * 8 + (SAMPLE_BINS + 1 + (vocab + part - 1) / part) * 4);
 }
@@ -655,7 +661,7 @@ extern "C" int posit_sample(void* stream, int fz, int64_t rows, int64_t vocab, c
     hipStream_t st = (hipStream_t)stream;
     discard_stale_hip_error();
     Sample a = {logits, u, temperature, top_p, min_p, top_k, token, kept, logprob, vocab, ldz, sample_shift(vocab), elem_fmt(fz), 0, 0, nullptr, nullptr, nullptr};
-    if (const int64_t part = sample_part(rows, vocab)) {
+    if (const int64_t part = sample_part(fz, rows, vocab)) {
         a.parts = (int)((vocab + part - 1) / part);
         a.weights = (unsigned long long*)workspace;
         a.counts = (uint32_t*)(a.weights + rows * SAMPLE_BINS);

@@ -38,6 +38,20 @@ def test_masked_logits_are_in_no_bin(bins, vocab, allowed, temperature):
         assert (eights == one).any(axis=1).sum() <= (b[at] == one).sum()
 
 
+def test_rows_of_8_bits_go_whole_while_registers_hold_them():
+    """They are counted, not weighed: nothing for other workgroups to share.  Of 16 bits few long rows go in parts, which need a workspace."""
+    from paper_2105_00053_amd import build, generate
+    if not os.path.exists(build.LIB):
+        build.build()
+    need = generate._load().posit_sample_workspace
+    for fz in (0, 3, 4):  # posit<8,0>, (8,1), (8,2)
+        for rows, vocab in ((1, 16385), (1, 50021), (32, 50021), (1, 131072), (64, 131072), (64, 150001), (128, 300007)):
+            assert need(fz, rows, vocab) == 0, (fz, rows, vocab)
+        assert need(fz, 1, 131073) > 0 and need(fz, 8, 200003) > 0
+    for fz in (1, 102, 100):
+        assert need(fz, 1, 16385) > 0 and need(fz, 32, 50021) > 0 and need(fz, 1, 16384) == 0 and need(fz, 128, 50021) == 0
+
+
 def test_bins_fall_with_the_logits(bins):
     z = np.sort(np.concatenate([np.random.default_rng(1).standard_normal(3000) * 30, [3.4e38, 1e20, -1e20, -3.4e38, 0.0, -0.0]]))[::-1]
     for temperature in (0.0, 1e-30, 0.05, 1.0, 1e30, np.inf):
