@@ -50,7 +50,7 @@ __device__ __forceinline__ void append_head(T (&x)[8], const float (&v)[8], cons
 
 // A block of rows to a workgroup; 8 or 16 lanes take a head, eight elements to each: of queries and keys four pairs that are rotated, of values and for the cache eight in a row.
 // Queries, keys and values are a pass each; of few rows each pass's rounds go to workgroups of their own (gridDim.y).
-// Bound by the vector unit, 66 % busy: keys in binary64, conversions of queries.  9 prompts of up to 2048 tokens, 32 + 8 heads of 128, posit<8,2> to bfloat16 and 4 bits: 108 to 111 us, where
+// Bound by the vector unit, 66 % busy: keys in binary64, conversions of queries.  9 prompts of up to 2048 tokens, 32 + 8 heads of 128, posit<8,2> to bfloat16 and 4 bits: 108 to 112 us, where
 // memory would take about 40; 4 tokens 6 us.
 template <int L, int KC, int KX, bool NEIGHBOURS, bool WHOLE>
 __global__ __launch_bounds__(256, 3) void cache_append_kernel(Append a) {

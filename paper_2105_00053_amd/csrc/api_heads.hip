@@ -44,7 +44,7 @@ __device__ __forceinline__ void heads_pairs(float2 (&cs)[4], const float2* row, 
 }
 
 // Memory's time would be the least (a head is read and written once); what is longer is the vector unit's: eight elements are looked up, squared, scaled, turned and rounded in some 130
-// instructions.  16384 rows of 32 + 8 heads of 128, posit<8,2> to bfloat16: 79 to 83 us.
+// instructions.  16384 rows of 32 + 8 heads of 128, posit<8,2> to bfloat16: 79 to 85 us.
 template <int L, bool NEIGHBOURS, bool WHOLE, int KX>
 __global__ __launch_bounds__(256, 4) void heads_fwd_kernel(Heads a) {
     __shared__ float2 angles[HEADS_BLOCK * 128];
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256, 4) void heads_fwd_kernel(Heads a) {
     }
 }
 
-// The same bound; dw adds nothing to memory, a lane's pairs being its own: one line a workgroup at the end.  The same sizes: 90 to 97 us.
+// The same bound; dw adds nothing to memory, a lane's pairs being its own: one line a workgroup at the end.  The same sizes: 90 to 101 us.
 template <int L, bool NEIGHBOURS, bool WHOLE, int KX>
 __global__ __launch_bounds__(256, 4) void heads_bwd_kernel(Heads a) {
     __shared__ float2 angles[HEADS_BLOCK * 128];

@@ -609,7 +609,7 @@ inline int sample_shift(int64_t vocab) {
 
 // Logits of a part, 0: rows are taken whole.  Parts pay where rows are long and few: they spread the weights over the chip, for two launches more.  All limits, us whole and in parts:
 // posit<16,1>: 1 x 20011 27 and 30, 1 x 32003 33 and 33, 1 x 50021 40 and 34, 32 x 50021 47 and 44, 128 x 50021 50 and 62, 1 x 131072 79 and 46, 64 x 100003 85 and 78, 128 x 131072 98 and 106; binary32:
-// 1 x 20011 26 and 30, 1 x 32003 33 and 33, 8 x 20011 61 and 60, 1 x 50021 48 and 38, 32 x 50021 276 and 209; bfloat16 between these.  So the 3 to 4 us of a single row of less than 32000 are lost.
+// 1 x 20011 26 and 30, 1 x 32003 33 and 33, 8 x 20011 61 and 60, 1 x 50021 48 and 38, 32 x 50021, rows at temperature 0 among them, 276 and 209; bfloat16 between these.  So the 3 to 4 us of a single row of less than 32000 are lost.
 // 8-bit posits are counted without weights, and whole is the faster as long as a row fits the registers: 1 x 20011 29 and 36, 32 x 50021 43 and 49, 1 x 131072 40 and 40, 64 x 100003 65 and 77; behind that
 // 1 x 150001 53 and 47, 8 x 200003 89 and 80, 64 x 150001 100 and 108, 128 x 300007 173 and 212.
 inline int64_t sample_part(int fz, int64_t rows, int64_t vocab) {

@@ -69,7 +69,7 @@ __device__ __forceinline__ float max_rows(float v) {
     return fmaxf(f32_of_bits(r.x), f32_of_bits(r.y));
 }
 
-// Bound by memory where lengths are alike (64 x 8192, 32 heads on 8 of 128, 4 bits: 5.0 TB/s), by the longest's end where not (the same up to 8192: 83 us with its join), by the chain of table, loads,
+// Bound by memory where lengths are alike (64 x 8192, 32 heads on 8 of 128, 4 bits: 571 MB in 126 us, 4.5 TB/s), by the longest's end where not (the same up to 8192: 83 us with its join), by the chain of table, loads,
 // products and joins where keys are few (3 x 300: 8.8 us).  Of 4 rows to a group the shared scores made 94 us of 155.
 // ROWS: of a block (4, 8 or 16).  The first product has 16 columns, one to a lane of 16, and four lanes have a column; of fewer rows the scores go to the lanes whose columns
 // are none, so that each works on 8 ROWS / 16 of them.  FULL: heads of 32 DB elements.
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256, KC == CACHE_BF16 ? 2 : 3) void attn_paged_kern
     at_store8(a.o, to * D + d, D - d < NV ? D - d : NV, a.ko, a.fo, out);
 }
 
-// Latency: the parts' maxima, then their rows with all loads in flight; 1 x 60000, 96 parts: 5 us.
+// Latency: the parts' maxima, then their rows with all loads in flight; 1 x 60000, 94 parts: 5 us.
 // Parts of a row joined, one row to a workgroup, an element to a thread of each four, which take the parts in turn; rows whose keys are in one part are done.
 __global__ __launch_bounds__(512) void attn_paged_join_kernel(AttnPaged a) {
     __shared__ float weight[AT_MOST_PARTS];
